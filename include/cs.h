@@ -50,7 +50,7 @@ typedef enum {
     CS_ERR_TIMEOUT = 7      /* device check: a bounded wait inside a kernel gave up */
 } cs_status;
 
-typedef enum { CS_F32 = 0, CS_BF16 = 1 } cs_dtype;
+typedef enum { CS_F32 = 0, CS_BF16 = 1, CS_MX4 = 2 /* blocks of four-bit elements: the cs_mx_ calls */ } cs_dtype;
 
 /* Shape of one FFN layer and of the recovery problem; fixed for the life of a plan. */
 typedef struct {
@@ -327,6 +327,82 @@ cs_status cs_prompt_support(cs_plan *plan, const float *S, const float *Phi, flo
  */
 cs_status cs_ffn_exec_shared(cs_plan *plan, const cs_layer *layer, const void *H, int32_t n,
                              const int32_t *support, void *out, void *stream);
+
+/*
+ * Microscaled low precision: weights in four bits, activations in eight, in blocks of 32 consecutive elements that share a
+ * power of two (the OCP layouts mxfp4 and mxfp8).  A plan for it has w_dtype = CS_MX4, group = 128 and d a multiple of 128
+ * (CS_ERR_UNSUPPORTED otherwise); its sensor and estimator calls are those of any plan, its actuator is cs_mx_ffn /
+ * cs_mx_ffn_shared, and the calls that take a cs_layer return CS_ERR_UNSUPPORTED.  One layer of a decode step:
+ *     cs_mx_norm (residual, n, q, s) -> cs_sketch(n) -> cs_recover -> cs_mx_ffn(q, s) -> the next cs_mx_norm's delta.
+ *
+ * A block whose largest magnitude is amax has the scale 2^e, e the smallest integer >= -127 with amax <= M 2^e, where M is
+ * the element type's largest value (e2m1: 6, e4m3: 448); it is stored as the byte e + 127.  Elements are x 2^-e rounded to
+ * nearest, ties to even: no element saturates.  A block that holds a NaN or an infinity gets the byte 255 and stands for NaN.
+ */
+
+/* A matrix [rows, cols] of four-bit elements, row-major: codes [rows, 16 ceil(cols/32)] bytes, two elements to a byte, the
+ * even one in the low half; scales [rows, ceil(cols/32)] bytes.  Elements of the last block behind `cols` are 0. */
+typedef struct {
+    const uint8_t *codes, *scales;
+} cs_mx_matrix;
+
+/*
+ * Quantises w (f32 or bf16, rows of `ld` >= cols elements).  transpose != 0: the result is that of the transpose, a matrix
+ * [cols, rows] with blocks down the columns of w (the framework's Wd_t [d_ff, d] becomes W_down [d, d_ff]).  No plan is
+ * needed.  codes must be 16-byte aligned (CS_ERR_UNSUPPORTED); ld < cols, an empty matrix, more than 2^29 blocks or, with
+ * transpose, more than 2^24 - 256 rows: CS_ERR_SHAPE.
+ */
+cs_status cs_mx_quantize(const void *w, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, int32_t transpose,
+                         uint8_t *codes, uint8_t *scales, void *stream);
+
+/* The values codes and scales stand for, as f32 or bf16 (exact in both, but for magnitudes of 2^128 and more, which become
+ * infinities: those above 3.5 * 2^126 are quantised to 2^128), rows of `ld` >= cols elements.  Refusals as above. */
+cs_status cs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int32_t rows, int32_t cols, int32_t dtype, void *w,
+                           int64_t ld, void *stream);
+
+/* Weights of one layer in the order cs_mx_ffn reads them (device pointers, caller-owned, written by cs_mx_pack): tiles of
+ * 128 rows x 128 columns, the codes row by row (8192 bytes), the scales in tile order (512 bytes, see cs_mx_norm).
+ * gate_up: for each 64 channels, for each 128 columns, a tile of 64 rows of W_gate and the same 64 of W_up.
+ * down: for each 128 rows of W_down [d, d_ff], for each group, a tile.  Codes are 32-byte, scales 16-byte aligned. */
+typedef struct {
+    const uint8_t *gate_up_codes;   /* [d_ff * d]       bytes */
+    const uint8_t *gate_up_scales;  /* [d_ff * d / 16]  */
+    const uint8_t *down_codes;      /* [d_ff * d / 2]   */
+    const uint8_t *down_scales;     /* [d_ff * d / 32]  */
+} cs_mx_layer;
+
+/* Lays out gate and up [d_ff, d] and down [d, d_ff] as above. */
+cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_matrix *up, const cs_mx_matrix *down,
+                     uint8_t *gate_up_codes, uint8_t *gate_up_scales, uint8_t *down_codes, uint8_t *down_scales, void *stream);
+
+/*
+ * What stands in front of the FFN of a layer:  h = x + delta, rounded to x's type (delta NULL: h = x);
+ * n = h / sqrt(mean(h^2) + rms_eps) * gamma (gamma NULL: 1), in f32;  q, s = n in blocks of e4m3.
+ *   x [B,d] f32 or bf16, delta [B,d] f32 or bf16 (the output of the block before), gamma [d] f32
+ *   -> x_out [B,d] of x's type (may be x or NULL), n_out [B,d] f32 or NULL (what cs_sketch reads), q [B,d] e4m3 bytes,
+ *   s [ceil(B/128), d/128, 512] bytes: the scale of row r, block b at byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of tile
+ *   (r / 128, b / 4), the order in which block-scaled tensor-core products read scales; scales of rows from B on are 0.
+ * A NaN makes its row NaN, an infinity its block (the rest of such a row is 0); rows keep to themselves.  Other than x_out = x (and delta = n_out or x_out), outputs overlap no input.
+ * Pointers are 16-byte aligned.  No scratch of the plan is used.
+ */
+cs_status cs_mx_norm(cs_plan *plan, const void *x, int32_t x_dtype, const void *delta, int32_t delta_dtype, const float *gamma,
+                     int32_t B, void *x_out, float *n_out, uint8_t *q, uint8_t *s, void *stream);
+
+/*
+ * The actuator of cs_ffn_exec on such operands: with n = q s and the weights' values,
+ *   a[c]   = silu(W_gate[c,:] . n_t) * (W_up[c,:] . n_t)   for every channel c of a group in s_t, in f32,
+ *   a^     = a in blocks of 32 channels of e4m3 (four blocks to a group),
+ *   out[t] = sum_c a^[c] W_down[:, c], accumulated in f32 and rounded to bf16.
+ *   q, s as cs_mx_norm leaves them (scales of rows from B on are read and may be anything), support [B,k] int32 as cs_ffn_exec
+ *   (checked on the device; an index outside [0,G) counts for nothing) -> out [B,d] bf16.
+ * Rows are independent, but weights that stand for NaN reach every token of a call whose union of supports holds their group.
+ */
+cs_status cs_mx_ffn(cs_plan *plan, const cs_mx_layer *layer, const uint8_t *q, const uint8_t *s, const int32_t *support,
+                    int32_t B, void *out, void *stream);
+
+/* The same for n tokens that share one support [k] (cs_prompt_support's, or any other). */
+cs_status cs_mx_ffn_shared(cs_plan *plan, const cs_mx_layer *layer, const uint8_t *q, const uint8_t *s, const int32_t *support,
+                           int32_t n, void *out, void *stream);
 
 /*
  * cs_layer_step for callers whose activations live in HOST memory (ideally pinned): copies

@@ -12,7 +12,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libcs_b200.so")
 _HEADER = os.path.join(os.path.dirname(_PKG), "include", "cs.h")
 
-CS_F32, CS_BF16 = 0, 1
+CS_F32, CS_BF16, CS_MX4 = 0, 1, 2
+_DTYPES = {torch.float32: CS_F32, torch.bfloat16: CS_BF16}
 _STATUS_NAMES = {0: "CS_OK", 1: "CS_ERR_NULL", 2: "CS_ERR_SHAPE", 3: "CS_ERR_UNSUPPORTED",
                  4: "CS_ERR_SUPPORT", 5: "CS_ERR_NONFINITE", 6: "CS_ERR_CUDA", 7: "CS_ERR_TIMEOUT"}
 
@@ -34,6 +35,15 @@ class _StepOptions(ctypes.Structure):
                 ("z_prev", ctypes.c_void_p), ("warm_start", ctypes.c_int32), ("gamma", ctypes.c_float),
                 ("reuse_support", ctypes.c_int32), ("srht_sign", ctypes.c_void_p), ("srht_rows", ctypes.c_void_p),
                 ("delta_out", ctypes.c_void_p), ("drift_out", ctypes.c_void_p)]
+
+
+class _MxMatrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class _MxLayer(ctypes.Structure):
+    _fields_ = [("gate_up_codes", ctypes.c_void_p), ("gate_up_scales", ctypes.c_void_p),
+                ("down_codes", ctypes.c_void_p), ("down_scales", ctypes.c_void_p)]
 
 
 SOLVERS = {"iht": 0, "niht": 1, "omp": 2}
@@ -100,6 +110,15 @@ def load_library():
     lib.cs_ffn_exec_static.restype = ctypes.c_int
     lib.cs_bucket.argtypes = [vp, vp, i32, vp, vp, vp, vp]
     lib.cs_bucket.restype = ctypes.c_int
+    i64, mat = ctypes.c_int64, ctypes.POINTER(_MxMatrix)
+    lib.cs_mx_quantize.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
+    lib.cs_mx_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp]
+    lib.cs_mx_pack.argtypes = [vp, mat, mat, mat, vp, vp, vp, vp, vp]
+    lib.cs_mx_norm.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp]
+    lib.cs_mx_ffn.argtypes = [vp, ctypes.POINTER(_MxLayer), vp, vp, vp, i32, vp, vp]
+    lib.cs_mx_ffn_shared.argtypes = [vp, ctypes.POINTER(_MxLayer), vp, vp, vp, i32, vp, vp]
+    for name in ("cs_mx_quantize", "cs_mx_dequantize", "cs_mx_pack", "cs_mx_norm", "cs_mx_ffn", "cs_mx_ffn_shared"):
+        getattr(lib, name).restype = ctypes.c_int
     lib.cs_last_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.cs_launch_count.argtypes = [vp]
     lib.cs_launch_count.restype = ctypes.c_int64
@@ -145,9 +164,10 @@ def _stream(stream) -> int:
 
 
 class Plan:
-    """Owns a cs_plan (device scratch sized for one layer shape)."""
+    """Owns a cs_plan (device scratch sized for one layer shape).  w_dtype: torch.float32, torch.bfloat16, or "mx4" for
+    weights in blocks of four-bit elements (the cs_mx_ calls)."""
 
-    def __init__(self, d: int, d_ff: int, group: int, m: int, k: int, T: int, w_dtype: torch.dtype,
+    def __init__(self, d: int, d_ff: int, group: int, m: int, k: int, T: int, w_dtype,
                  max_tokens: int, rms_eps: float = 1e-5):
         self.lib = load_library()
         self.d, self.d_ff, self.group, self.m, self.k, self.T = d, d_ff, group, m, k, T
@@ -155,7 +175,7 @@ class Plan:
         self.w_dtype = w_dtype
         self.max_tokens = max_tokens
         self._templates = {}
-        code = {torch.float32: CS_F32, torch.bfloat16: CS_BF16}.get(w_dtype, -1)
+        code = CS_MX4 if w_dtype == "mx4" else _DTYPES.get(w_dtype, -1)
         cfg = _Config(d, d_ff, group, m, k, T, code, max_tokens, rms_eps)
         handle = ctypes.c_void_p()
         st = self.lib.cs_plan_create(ctypes.byref(cfg), ctypes.byref(handle))
@@ -487,3 +507,130 @@ def cs_ffn_exec_shared(plan: Plan, layer: Layer, H, support, out=None, stream=No
                                            _ptr(out, torch.bfloat16, "out", (n, plan.d)), _stream(stream)),
                "cs_ffn_exec_shared")
     return out
+
+
+# ---- microscaled low precision ---------------------------------------------------------------------
+
+_BYTES = (torch.uint8, torch.float8_e8m0fnu, torch.float8_e4m3fn)
+
+
+def _on_current_device(*tensors):
+    """The calls enqueue on the current device's stream: a tensor of another device must not reach them."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != device:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{device}")
+
+
+def _byte_ptr(t: torch.Tensor, name: str, shape) -> int:
+    """A tensor of one-byte elements (uint8, or the float8 type they are): the pointer."""
+    if t.dtype not in _BYTES:
+        raise TypeError(f"{name} must hold bytes (uint8, float8_e8m0fnu or float8_e4m3fn), got {t.dtype}")
+    return _ptr(t, t.dtype, name, shape)
+
+
+def _dtype_code(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def cs_mx_quantize(w, transpose: bool = False, codes=None, scales=None, stream=None):
+    """w [rows, cols] f32 or bf16, rows contiguous (any row stride) -> (codes [rows, 16 ceil(cols/32)] uint8, scales
+    [rows, ceil(cols/32)] float8_e8m0fnu): blocks of 32 four-bit elements.  transpose: those of the transpose (Wd_t ->
+    W_down)."""
+    lib = load_library()
+    if w.dim() != 2 or not w.is_cuda:
+        raise TypeError("w must be a CUDA matrix")
+    rows, cols = w.shape
+    if rows == 0 or cols == 0:
+        raise ValueError("w is empty")
+    if cols > 1 and w.stride(1) != 1:
+        raise ValueError("w must have contiguous rows")
+    ld = w.stride(0) if rows > 1 else cols
+    n, nb = (cols, -(-rows // 32)) if transpose else (rows, -(-cols // 32))
+    codes = torch.empty((n, 16 * nb), dtype=torch.uint8, device=w.device) if codes is None else codes
+    scales = torch.empty((n, nb), dtype=torch.float8_e8m0fnu, device=w.device) if scales is None else scales
+    _on_current_device(w, codes, scales)
+    st = lib.cs_mx_quantize(w.data_ptr(), _dtype_code(w, "w"), rows, cols, ld, int(bool(transpose)),
+                            _ptr(codes, torch.uint8, "codes", (n, 16 * nb)), _byte_ptr(scales, "scales", (n, nb)), _stream(stream))
+    if st != 0:
+        raise CSError(st, "cs_mx_quantize")
+    return codes, scales
+
+
+def cs_mx_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, stream=None):
+    """The values [rows, cols] of cs_mx_quantize's codes and scales, as f32 or bf16."""
+    lib = load_library()
+    if codes.dim() != 2:
+        raise ValueError("codes must be a matrix")
+    rows, nb = codes.shape[0], -(-cols // 32)
+    out = torch.empty((rows, cols), dtype=dtype, device=codes.device) if out is None else out
+    if tuple(out.shape) != (rows, cols) or not out.is_cuda or (cols > 1 and out.stride(1) != 1):
+        raise ValueError(f"out must be a CUDA matrix of shape ({rows}, {cols}) with contiguous rows")
+    _on_current_device(codes, scales, out)
+    st = lib.cs_mx_dequantize(_ptr(codes, torch.uint8, "codes", (rows, 16 * nb)), _byte_ptr(scales, "scales", (rows, nb)), rows, cols,
+                              _dtype_code(out, "out"), out.data_ptr(), out.stride(0) if rows > 1 else cols, _stream(stream))
+    if st != 0:
+        raise CSError(st, "cs_mx_dequantize")
+    return out
+
+
+class MxLayer:
+    """Weights of one layer in the order cs_mx_ffn reads them.  gate, up: (codes, scales) of [d_ff, d] matrices; down: of
+    W_down [d, d_ff] (cs_mx_quantize(Wd_t, transpose=True)).  They are copied; keeps its own tensors alive."""
+
+    def __init__(self, plan: Plan, gate, up, down, stream=None):
+        d, d_ff = plan.d, plan.d_ff
+
+        def matrix(pair, name, rows, cols):
+            return _MxMatrix(_ptr(pair[0], torch.uint8, name + " codes", (rows, cols // 2)),
+                             _byte_ptr(pair[1], name + " scales", (rows, cols // 32)))
+        _on_current_device(*gate, *up, *down)
+        ms = matrix(gate, "gate", d_ff, d), matrix(up, "up", d_ff, d), matrix(down, "down", d, d_ff)
+        n = d * d_ff
+        self.tensors = tuple(torch.empty((size,), dtype=torch.uint8, device=gate[0].device) for size in (n, n // 16, n // 2, n // 32))
+        self.c = _MxLayer(*(t.data_ptr() for t in self.tensors))
+        self.ref = ctypes.byref(self.c)
+        plan.check(plan.lib.cs_mx_pack(plan.handle, *(ctypes.byref(m) for m in ms), *(t.data_ptr() for t in self.tensors),
+                                       _stream(stream)), "cs_mx_pack")
+
+
+def cs_mx_norm(plan: Plan, x, gamma=None, delta=None, want_n: bool = False, x_out=None, stream=None):
+    """h = x + delta, n = RMSNorm(h) * gamma, in blocks of 32 e4m3 elements.  Returns (h, q [B, d] float8_e4m3fn, s
+    [ceil(B/128), d/128, 32, 4, 4] float8_e8m0fnu, n or None); h is x itself without a delta and x_out.  s is in tile order: the scale
+    of row r, block b stands at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4]."""
+    B, d = x.shape[0], plan.d
+    dev = x.device
+    _on_current_device(x, delta, gamma, x_out)
+    if x_out is None and delta is not None:
+        x_out = torch.empty_like(x)
+    n = torch.empty((B, d), dtype=torch.float32, device=dev) if want_n else None
+    q = torch.empty((B, d), dtype=torch.float8_e4m3fn, device=dev)
+    s = torch.empty((-(-B // 128), d // 128, 32, 4, 4), dtype=torch.float8_e8m0fnu, device=dev)
+    code = _dtype_code(x, "x")
+    plan.check(plan.lib.cs_mx_norm(plan.handle, _ptr(x, x.dtype, "x", (B, d)), code,
+                                   None if delta is None else _ptr(delta, delta.dtype, "delta", (B, d)),
+                                   0 if delta is None else _dtype_code(delta, "delta"),
+                                   _ptr(gamma, torch.float32, "gamma", (d,)), B, _ptr(x_out, x.dtype, "x_out", (B, d)),
+                                   None if n is None else n.data_ptr(), q.data_ptr(), s.data_ptr(), _stream(stream)), "cs_mx_norm")
+    return (x if x_out is None else x_out), q, s, n
+
+
+def _mx_ffn(call, name, plan: Plan, layer: MxLayer, q, s, support, support_shape, out, stream):
+    B, d = q.shape[0], plan.d
+    out = torch.empty((B, d), dtype=torch.bfloat16, device=q.device) if out is None else out
+    _on_current_device(q, s, support, out)
+    plan.check(call(plan.handle, layer.ref, _byte_ptr(q, "q", (B, d)), _byte_ptr(s, "s", (-(-B // 128), d // 128, 32, 4, 4)),
+                    _ptr(support, torch.int32, "support", support_shape), B, _ptr(out, torch.bfloat16, "out", (B, d)), _stream(stream)), name)
+    return out
+
+
+def cs_mx_ffn(plan: Plan, layer: MxLayer, q, s, support, out=None, stream=None):
+    """The FFN of B tokens on four-bit weights over the groups of support [B, k]; q, s from cs_mx_norm.  Returns out [B, d] bf16."""
+    return _mx_ffn(plan.lib.cs_mx_ffn, "cs_mx_ffn", plan, layer, q, s, support, (q.shape[0], plan.k), out, stream)
+
+
+def cs_mx_ffn_shared(plan: Plan, layer: MxLayer, q, s, support, out=None, stream=None):
+    """The same for tokens that share one support [k]."""
+    return _mx_ffn(plan.lib.cs_mx_ffn_shared, "cs_mx_ffn_shared", plan, layer, q, s, support, (plan.k,), out, stream)

@@ -5,7 +5,7 @@
 
 #include <new>
 
-#include "cs_internal.cuh"
+#include "mx.cuh"
 
 namespace cs {
 
@@ -24,7 +24,8 @@ static cs_status check_config(const cs_config *c) {
     if (!(c->rms_eps > 0.f) || !isfinite(c->rms_eps)) return CS_ERR_NONFINITE;
     if (c->group != 64 && c->group != 128) return CS_ERR_UNSUPPORTED;
     if (G > kMaxG || c->m > kMaxM || c->d > kMaxD || c->d % 64 != 0) return CS_ERR_UNSUPPORTED;
-    if (c->w_dtype != CS_F32 && c->w_dtype != CS_BF16) return CS_ERR_UNSUPPORTED;
+    if (c->w_dtype != CS_F32 && c->w_dtype != CS_BF16 && c->w_dtype != CS_MX4) return CS_ERR_UNSUPPORTED;
+    if (c->w_dtype == CS_MX4 && (c->group != 128 || c->d % 128 != 0)) return CS_ERR_UNSUPPORTED;
     return CS_OK;
 }
 
@@ -81,7 +82,8 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
     alloc((void **)&p->n_buf, nt * cfg->d * sizeof(float));
     alloc((void **)&p->y_buf, nt * cfg->m * sizeof(float));
     alloc((void **)&p->sup_buf, nt * cfg->k * sizeof(int32_t));
-    alloc((void **)&p->partial, (size_t)kGatherMaxTokens * p->nx_max * cfg->d * sizeof(float));
+    const bool mx = cfg->w_dtype == CS_MX4;
+    if (!mx) alloc((void **)&p->partial, (size_t)kGatherMaxTokens * p->nx_max * cfg->d * sizeof(float));
     alloc((void **)&p->gram, (size_t)kMaxG * kMaxG * sizeof(float));
     alloc((void **)&p->resid_buf, nt * sizeof(float));
     alloc((void **)&p->fb_flags, nt * sizeof(int32_t));
@@ -116,8 +118,13 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
         const size_t decode_rows = (size_t)decode_slices(p) * min(nt, (size_t)kDecodeMaxTokens);
         alloc((void **)&p->mma_partial, max(max(slice_rows, max(decode_rows, 2 * min(nt, (size_t)kDecodeMaxTokens))), m_pad) * cfg->d * sizeof(float));
     }
-    alloc((void **)&p->x_host_in, nt * cfg->d * sizeof(float));
-    alloc((void **)&p->x_host_out, nt * cfg->d * sizeof(float));
+    if (mx) {
+        alloc((void **)&p->mx_a, nt * cfg->d_ff);
+        alloc((void **)&p->mx_a_scales, (nt + 127) / 128 * p->G * kMxTileBytes);
+    } else {
+        alloc((void **)&p->x_host_in, nt * cfg->d * sizeof(float));
+        alloc((void **)&p->x_host_out, nt * cfg->d * sizeof(float));
+    }
     for (int i = 0; i < 2 * CS_STAGE_COUNT; ++i)
         if (e == cudaSuccess) e = cudaEventCreate(&p->ev[i]);
     if (e == cudaSuccess) e = cudaMemset(p->status, 0, sizeof(DeviceStatus));
@@ -128,7 +135,8 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
     if (e == cudaSuccess && prepare_recover(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && prepare_prompt(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && prepare_solvers(p) != CS_OK) e = cudaErrorUnknown;
-    if (e == cudaSuccess && prepare_ffn_gather(p) != CS_OK) e = cudaErrorUnknown;
+    if (e == cudaSuccess && !mx && prepare_ffn_gather(p) != CS_OK) e = cudaErrorUnknown;
+    if (e == cudaSuccess && mx && prepare_mx_ffn(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && p->mma_ok && prepare_ffn_mma(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && p->mma_ok && prepare_decode(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess) e = cudaMemset(p->mask, 0, nt * 4 * sizeof(uint32_t));
@@ -147,6 +155,7 @@ cs_status cs_plan_destroy(cs_plan *p) {
     cudaFree(p->resid_buf); cudaFree(p->fb_flags); cudaFree(p->fb_list); cudaFree(p->fb_count); cudaFree(p->colsum);
     cudaFree(p->status); cudaFree(p->x_host_in); cudaFree(p->x_host_out);
     cudaFree(p->mask); cudaFree(p->mask_count); cudaFree(p->counts); cudaFree(p->offsets); cudaFree(p->token_ids); cudaFree(p->glist);
+    cudaFree(p->mx_a); cudaFree(p->mx_a_scales);
     cudaFree(p->nu); cudaFree(p->x_bf16); cudaFree(p->act); cudaFree(p->mma_partial);
     for (int i = 0; i < 2 * CS_STAGE_COUNT; ++i)
         if (p->ev[i] != nullptr) cudaEventDestroy(p->ev[i]);
@@ -274,7 +283,8 @@ cs_status cs_uds_budget(cs_plan *plan, const float *logits, int32_t B, int32_t V
     return launch_uds_budget(plan, logits, B, V, m_base, gamma, m_min, m_max, H, m_t, static_cast<cudaStream_t>(stream));
 }
 
-static cs_status check_weights(const cs_layer *L) {
+static cs_status check_weights(const cs_plan *plan, const cs_layer *L) {
+    if (plan->cfg.w_dtype == CS_MX4) return CS_ERR_UNSUPPORTED;   // such a plan's layers are cs_mx_layer
     if (L == nullptr || L->W_gate == nullptr || L->W_up == nullptr || L->Wd_t == nullptr) return CS_ERR_NULL;
     if (!aligned16(L->W_gate) || !aligned16(L->W_up) || !aligned16(L->Wd_t)) return CS_ERR_UNSUPPORTED;
     return CS_OK;
@@ -313,7 +323,7 @@ static cs_status exec_dispatch(cs_plan *plan, const cs_layer *layer, const float
 cs_status cs_ffn_exec(cs_plan *plan, const cs_layer *layer, const float *h, const int32_t *support,
                       int32_t B, const float *residual, float *out, void *stream) {
     if (plan == nullptr || h == nullptr || support == nullptr || out == nullptr) return CS_ERR_NULL;
-    cs_status s = check_weights(layer);
+    cs_status s = check_weights(plan, layer);
     if (s != CS_OK) return s;
     if (B <= 0 || B > plan->cfg.max_tokens) return CS_ERR_SHAPE;
     if (!aligned16(h) || !aligned16(out) || (residual != nullptr && !aligned16(residual))) return CS_ERR_UNSUPPORTED;
@@ -351,7 +361,7 @@ static cs_status decode_step(cs_plan *plan, const cs_layer *layer, const float *
 cs_status cs_layer_step(cs_plan *plan, const cs_layer *layer, const float *x, int32_t B, float *x_out,
                         int32_t *support_out, float *z_out, float *resid_out, void *stream) {
     if (plan == nullptr || x == nullptr || x_out == nullptr) return CS_ERR_NULL;
-    cs_status s = check_weights(layer);
+    cs_status s = check_weights(plan, layer);
     if (s != CS_OK) return s;
     if (layer->S == nullptr || layer->Phi == nullptr) return CS_ERR_NULL;
     if (B <= 0 || B > plan->cfg.max_tokens) return CS_ERR_SHAPE;
@@ -400,7 +410,7 @@ cs_status cs_layer_step_ex(cs_plan *plan, const cs_layer *layer, const float *x,
                            float *resid_out, void *stream) {
     if (opt == nullptr) return cs_layer_step(plan, layer, x, B, x_out, support_out, z_out, resid_out, stream);
     if (plan == nullptr || x == nullptr || x_out == nullptr) return CS_ERR_NULL;
-    cs_status s = check_weights(layer);
+    cs_status s = check_weights(plan, layer);
     if (s != CS_OK) return s;
     const bool srht = opt->srht_sign != nullptr;
     if (layer->Phi == nullptr || (!srht && layer->S == nullptr)) return CS_ERR_NULL;
@@ -492,7 +502,7 @@ cs_status cs_layer_step_host(cs_plan *plan, const cs_layer *layer, const float *
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t bytes = (size_t)B * plan->cfg.d * sizeof(float);
     // validate before the first copy so that nothing is enqueued on an error
-    cs_status s = check_weights(layer);
+    cs_status s = check_weights(plan, layer);
     if (s != CS_OK) return s;
     if (layer->S == nullptr || layer->Phi == nullptr) return CS_ERR_NULL;
     if (!isfinite(layer->mu) || !(layer->mu > 0.f)) return CS_ERR_NONFINITE;
@@ -541,7 +551,7 @@ int32_t cs_plan_crossover(const cs_plan *plan) { return plan != nullptr ? plan->
 
 cs_status cs_plan_set_speculative(cs_plan *plan, int32_t on) {
     if (plan == nullptr) return CS_ERR_NULL;
-    if (on && !sketch_recover_ok(plan)) return CS_ERR_UNSUPPORTED;
+    if (on && (!sketch_recover_ok(plan) || plan->cfg.w_dtype == CS_MX4)) return CS_ERR_UNSUPPORTED;
     if (on < 0 || on > 2) return CS_ERR_SHAPE;
     plan->speculative = on;
     return CS_OK;
@@ -580,12 +590,46 @@ cs_status cs_prompt_support(cs_plan *plan, const float *S, const float *Phi, flo
 cs_status cs_ffn_exec_shared(cs_plan *plan, const cs_layer *layer, const void *H, int32_t n,
                              const int32_t *support, void *out, void *stream) {
     if (plan == nullptr || H == nullptr || support == nullptr || out == nullptr) return CS_ERR_NULL;
-    cs_status s = check_weights(layer);
+    cs_status s = check_weights(plan, layer);
     if (s != CS_OK) return s;
     if (n <= 0 || n > plan->cfg.max_tokens) return CS_ERR_SHAPE;
     if (!plan->mma_ok || !aligned16(H) || !aligned16(out)) return CS_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return launch_ffn_mma(plan, layer, H, nullptr, n, support, nullptr, plan->cfg.k, nullptr, nullptr, nullptr, out, st);   // checks the support
+}
+
+cs_status cs_mx_norm(cs_plan *plan, const void *x, int32_t x_dtype, const void *delta, int32_t delta_dtype, const float *gamma,
+                     int32_t B, void *x_out, float *n_out, uint8_t *q, uint8_t *s, void *stream) {
+    if (plan == nullptr || x == nullptr || q == nullptr || s == nullptr) return CS_ERR_NULL;
+    if (B <= 0 || B > plan->cfg.max_tokens) return CS_ERR_SHAPE;
+    if (plan->cfg.w_dtype != CS_MX4 || (x_dtype != CS_F32 && x_dtype != CS_BF16) ||
+        (delta != nullptr && delta_dtype != CS_F32 && delta_dtype != CS_BF16))
+        return CS_ERR_UNSUPPORTED;
+    for (const void *p : {x, delta, static_cast<const void *>(gamma), static_cast<const void *>(x_out), static_cast<const void *>(n_out),
+                          static_cast<const void *>(q), static_cast<const void *>(s)})
+        if (!aligned16(p)) return CS_ERR_UNSUPPORTED;
+    return launch_mx_norm(plan, x, x_dtype, delta, delta_dtype, gamma, B, x_out, n_out, q, s, static_cast<cudaStream_t>(stream));
+}
+
+static cs_status mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const uint8_t *s, const int32_t *support, bool shared, int32_t B,
+                        void *out, void *stream) {
+    if (plan == nullptr || L == nullptr || q == nullptr || s == nullptr || support == nullptr || out == nullptr) return CS_ERR_NULL;
+    if (L->gate_up_codes == nullptr || L->gate_up_scales == nullptr || L->down_codes == nullptr || L->down_scales == nullptr) return CS_ERR_NULL;
+    if (B <= 0 || B > plan->cfg.max_tokens) return CS_ERR_SHAPE;
+    if (plan->cfg.w_dtype != CS_MX4) return CS_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(s) || !aligned16(out) || !aligned16(L->gate_up_scales) || !aligned16(L->down_scales)) return CS_ERR_UNSUPPORTED;
+    if (((reinterpret_cast<uintptr_t>(L->gate_up_codes) | reinterpret_cast<uintptr_t>(L->down_codes)) & 31u) != 0) return CS_ERR_UNSUPPORTED;
+    return launch_mx_ffn(plan, L, q, s, support, shared, B, out, static_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_mx_ffn(cs_plan *plan, const cs_mx_layer *layer, const uint8_t *q, const uint8_t *s, const int32_t *support,
+                    int32_t B, void *out, void *stream) {
+    return mx_ffn(plan, layer, q, s, support, false, B, out, stream);
+}
+
+cs_status cs_mx_ffn_shared(cs_plan *plan, const cs_mx_layer *layer, const uint8_t *q, const uint8_t *s, const int32_t *support,
+                           int32_t n, void *out, void *stream) {
+    return mx_ffn(plan, layer, q, s, support, true, n, out, stream);
 }
 
 cs_status cs_last_device_status(cs_plan *plan, void *stream, int32_t *code) {

@@ -1,0 +1,293 @@
+// Weights to blocks of four-bit elements and back, and the order in which the FFN kernels read them.  See mx.cuh for the block format.
+//
+// All of it is bound by HBM: an element is read once (2 or 4 bytes) and written once (17/32 byte), or the reverse.
+#include "mx.cuh"
+
+namespace cs {
+
+namespace {
+
+constexpr int kQThreads = 256;
+constexpr int kQUnroll = 4;     // 16- or 32-byte chunks a thread has in flight
+
+template <typename T> __device__ __forceinline__ float widen(T v);
+template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
+template <> __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T narrow(float v);
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Eight consecutive elements, of which the first `n` exist.
+template <typename T, bool VEC> __device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
+    if (VEC) {
+        if (n <= 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            return;
+        }
+        if constexpr (sizeof(T) == 2) {
+            Chunk<__nv_bfloat16>::widen(__ldcs(reinterpret_cast<const uint4 *>(p)), v);
+        } else {
+            const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen<T>(p[i]) : 0.f;
+    }
+}
+
+// Four threads per block of 32 elements along the rows.  VEC: whole chunks of eight elements, 16-byte aligned.
+template <typename T, bool VEC> __global__ void __launch_bounds__(kQThreads)
+quantize_rows_kernel(const T *__restrict__ w, int rows, int cols, int64_t ld, uint32_t nb, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint32_t parts = (uint32_t)rows * nb * 4;      // the host bounds it by 2^31
+    const uint32_t base = blockIdx.x * (kQThreads * kQUnroll) + threadIdx.x;
+    float v[kQUnroll][8];
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+        const uint32_t i = base + u * kQThreads;
+        const uint32_t row = i / (4 * nb), part = i - row * (4 * nb);
+        load8<T, VEC>(w + (int64_t)row * ld + part * 8, i < parts ? cols - (int)part * 8 : 0, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+        const uint32_t i = base + u * kQThreads;
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[u][j]));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const uint32_t byte = mx_scale_byte<false>(m);
+        const float inv = mx_inverse(byte);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] = byte == 255 ? 0.f : v[u][j] * inv;
+        if (i < parts) {
+            reinterpret_cast<uint32_t *>(codes)[i] = pack_e2m1(v[u]);
+            if ((i & 3) == 0) scales[i >> 2] = (uint8_t)byte;
+        }
+    }
+}
+
+// Blocks down the columns, written as rows of the transpose.  A thread takes two columns of 32 rows (no exchange between threads); eight warps stand
+// below one another, so that a column's codes leave as 128 contiguous bytes through shared memory.
+constexpr int kTCols = 64, kTBlocks = 8;
+template <typename T, bool VEC> __global__ void __launch_bounds__(32 * kTBlocks)
+quantize_cols_kernel(const T *__restrict__ w, int rows, int cols, int64_t ld, int nb, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    __shared__ uint4 tile[kTCols][kTBlocks + 1];     // the odd pitch spreads a column of 16-byte cells over the banks
+    __shared__ uint8_t st[kTCols][kTBlocks];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * kTCols + 2 * lane, b = blockIdx.y * kTBlocks + warp, r0 = b * kMxBlock;
+    float v[2][kMxBlock];
+    const T *p = w + (int64_t)r0 * ld + c;
+#pragma unroll
+    for (int r = 0; r < kMxBlock; ++r) {
+        const bool row = r0 + r < rows;
+        if (VEC) {
+            v[0][r] = v[1][r] = 0.f;
+            if (row && c < cols) {
+                if constexpr (sizeof(T) == 2) {
+                    const uint32_t u = __ldcs(reinterpret_cast<const uint32_t *>(p + (int64_t)r * ld));
+                    v[0][r] = bf16_lo(u); v[1][r] = bf16_hi(u);
+                } else {
+                    const float2 u = __ldcs(reinterpret_cast<const float2 *>(p + (int64_t)r * ld));
+                    v[0][r] = u.x; v[1][r] = u.y;
+                }
+            }
+        } else {
+            v[0][r] = row && c < cols ? widen<T>(p[(int64_t)r * ld]) : 0.f;
+            v[1][r] = row && c + 1 < cols ? widen<T>(p[(int64_t)r * ld + 1]) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < kMxBlock; ++r) m = max(m, abs_bits(v[h][r]));
+        const uint32_t byte = mx_scale_byte<false>(m);
+        const float inv = mx_inverse(byte);
+        uint32_t q[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = byte == 255 ? 0.f : v[h][8 * g + j] * inv;
+            q[g] = pack_e2m1(e);
+        }
+        tile[2 * lane + h][warp] = make_uint4(q[0], q[1], q[2], q[3]);
+        st[2 * lane + h][warp] = (uint8_t)byte;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTCols * kTBlocks; i += 32 * kTBlocks) {
+        const int col = blockIdx.x * kTCols + i / kTBlocks, blk = blockIdx.y * kTBlocks + i % kTBlocks;
+        if (col < cols && blk < nb) {
+            reinterpret_cast<uint4 *>(codes)[(int64_t)col * nb + blk] = tile[i / kTBlocks][i % kTBlocks];
+            scales[(int64_t)col * nb + blk] = st[i / kTBlocks][i % kTBlocks];
+        }
+    }
+}
+
+// Eight codes to floats: two e2m1 become a pair of f16 (exactly), times the scale.
+__device__ __forceinline__ void unpack_e2m1(uint32_t q, float s, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h;
+        asm("{\n.reg .b8 a, b, c, d;\nmov.b32 {a, b, c, d}, %1;\ncvt.rn.f16x2.e2m1x2 %0, a;\n}" : "=r"(h) : "r"(q >> (8 * i)));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+        v[2 * i] = f.x * s; v[2 * i + 1] = f.y * s;
+    }
+}
+
+template <typename T, bool VEC> __global__ void __launch_bounds__(kQThreads)
+dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols, uint32_t nb, T *__restrict__ w, int64_t ld) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint32_t parts = (uint32_t)rows * nb * 4;
+    const uint32_t base = blockIdx.x * (kQThreads * kQUnroll) + threadIdx.x;
+    uint32_t q[kQUnroll]; uint32_t s[kQUnroll];
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+        const uint32_t i = base + u * kQThreads;
+        q[u] = 0; s[u] = 0;
+        if (i < parts) { q[u] = __ldcs(reinterpret_cast<const uint32_t *>(codes) + i); s[u] = __ldcs(scales + (i >> 2)); }
+    }
+#pragma unroll
+    for (int u = 0; u < kQUnroll; ++u) {
+        const uint32_t i = base + u * kQThreads;
+        if (i >= parts) break;
+        const uint32_t row = i / (4 * nb), part = i - row * (4 * nb);
+        T *p = w + (int64_t)row * ld + part * 8;
+        const int n = cols - (int)part * 8;
+        float v[8];
+        unpack_e2m1(q[u], mx_scale(s[u]), v);
+        if (VEC) {
+            if (n > 0) {
+                if constexpr (sizeof(T) == 2) {
+                    __nv_bfloat162 o[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                    *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(o);
+                } else {
+                    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) p[j] = narrow<T>(v[j]);
+        }
+    }
+}
+
+// Row-major codes and scales to the FFN's tiles of 128 rows x 128 columns (8 KB of codes, row by row, and 512 scales in tile order).
+// Gate and up share a tile: rows 0..63 are 64 channels of W_gate, rows 64..127 the same channels of W_up.
+__global__ void __launch_bounds__(256)
+pack_tiles_kernel(const uint8_t *__restrict__ c0, const uint8_t *__restrict__ s0, const uint8_t *__restrict__ c1, const uint8_t *__restrict__ s1,
+                  int kblocks, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t tile = blockIdx.x;                  // (row tile, k block), k block fastest
+    const int64_t rt = tile / kblocks;
+    const int kb = (int)(tile - rt * kblocks);
+    for (int i = threadIdx.x; i < 512; i += 256) {    // 128 rows x 4 chunks of 16 bytes
+        const int r = i >> 2;
+        const bool second = c1 != nullptr && r >= 64;
+        const int64_t row = c1 == nullptr ? rt * 128 + r : rt * 64 + (r & 63);
+        const uint8_t *src = (second ? c1 : c0) + (row * kblocks + kb) * 64;
+        reinterpret_cast<uint4 *>(codes + tile * 8192)[i] = reinterpret_cast<const uint4 *>(src)[i & 3];
+    }
+    if (threadIdx.x < 128) {
+        const int r = threadIdx.x;
+        const bool second = c1 != nullptr && r >= 64;
+        const int64_t row = c1 == nullptr ? rt * 128 + r : rt * 64 + (r & 63);
+        const uint32_t v = reinterpret_cast<const uint32_t *>(second ? s1 : s0)[row * kblocks + kb];
+        reinterpret_cast<uint32_t *>(scales + tile * kMxTileBytes)[(r & 31) * 4 + (r >> 5)] = v;
+    }
+}
+
+bool fits(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 && rows * ((cols + 31) / 32) * 4 < (int64_t)1 << 31; }
+bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+cs_status status_of(cudaError_t e) { return e == cudaSuccess ? CS_OK : CS_ERR_CUDA; }
+
+template <typename T> cs_status quantize(const T *w, int rows, int cols, int64_t ld, bool transpose, uint8_t *codes, uint8_t *scales, cudaStream_t st) {
+    if (transpose) {
+        const int nb = (rows + 31) / 32;
+        const dim3 grid((cols + kTCols - 1) / kTCols, (nb + kTBlocks - 1) / kTBlocks);
+        if (grid.y > 65535) return CS_ERR_SHAPE;
+        const bool vec = cols % 2 == 0 && ld % 2 == 0 && aligned(w, 2 * sizeof(T));
+        return status_of(launch_pdl(true, vec ? quantize_cols_kernel<T, true> : quantize_cols_kernel<T, false>, grid, dim3(32 * kTBlocks), 0, st, w, rows,
+                                    cols, ld, nb, codes, scales));
+    }
+    const uint32_t nb = (cols + 31) / 32;
+    const int64_t parts = (int64_t)rows * nb * 4;
+    const dim3 grid((unsigned)((parts + kQThreads * kQUnroll - 1) / (kQThreads * kQUnroll)));
+    const bool vec = cols % 8 == 0 && (ld * sizeof(T)) % 16 == 0 && aligned(w, 16);
+    return status_of(launch_pdl(true, vec ? quantize_rows_kernel<T, true> : quantize_rows_kernel<T, false>, grid, dim3(kQThreads), 0, st, w, rows, cols, ld,
+                                nb, codes, scales));
+}
+
+template <typename T> cs_status dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, T *w, int64_t ld, cudaStream_t st) {
+    const uint32_t nb = (cols + 31) / 32;
+    const int64_t parts = (int64_t)rows * nb * 4;
+    const dim3 grid((unsigned)((parts + kQThreads * kQUnroll - 1) / (kQThreads * kQUnroll)));
+    const bool vec = cols % 8 == 0 && (ld * sizeof(T)) % 16 == 0 && aligned(w, 16);
+    return status_of(launch_pdl(true, vec ? dequantize_kernel<T, true> : dequantize_kernel<T, false>, grid, dim3(kQThreads), 0, st, codes, scales, rows,
+                                cols, nb, w, ld));
+}
+
+}  // namespace
+
+}  // namespace cs
+
+using namespace cs;
+
+extern "C" {
+
+cs_status cs_mx_quantize(const void *w, int32_t dtype, int32_t rows, int32_t cols, int64_t ld, int32_t transpose, uint8_t *codes,
+                         uint8_t *scales, void *stream) {
+    if (w == nullptr || codes == nullptr || scales == nullptr) return CS_ERR_NULL;
+    if (dtype != CS_F32 && dtype != CS_BF16) return CS_ERR_UNSUPPORTED;
+    if (ld < cols || !fits(transpose ? cols : rows, transpose ? rows : cols)) return CS_ERR_SHAPE;
+    if (!aligned(codes, 16) || !aligned(w, dtype == CS_F32 ? 4 : 2)) return CS_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == CS_F32 ? quantize(static_cast<const float *>(w), rows, cols, ld, transpose != 0, codes, scales, st)
+                           : quantize(static_cast<const __nv_bfloat16 *>(w), rows, cols, ld, transpose != 0, codes, scales, st);
+}
+
+cs_status cs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int32_t rows, int32_t cols, int32_t dtype, void *w, int64_t ld,
+                           void *stream) {
+    if (w == nullptr || codes == nullptr || scales == nullptr) return CS_ERR_NULL;
+    if (dtype != CS_F32 && dtype != CS_BF16) return CS_ERR_UNSUPPORTED;
+    if (ld < cols || !fits(rows, cols)) return CS_ERR_SHAPE;
+    if (!aligned(codes, 16) || !aligned(w, dtype == CS_F32 ? 4 : 2)) return CS_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == CS_F32 ? dequantize(codes, scales, rows, cols, static_cast<float *>(w), ld, st)
+                           : dequantize(codes, scales, rows, cols, static_cast<__nv_bfloat16 *>(w), ld, st);
+}
+
+cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_matrix *up, const cs_mx_matrix *down, uint8_t *gate_up_codes,
+                     uint8_t *gate_up_scales, uint8_t *down_codes, uint8_t *down_scales, void *stream) {
+    if (plan == nullptr || gate == nullptr || up == nullptr || down == nullptr || gate_up_codes == nullptr || gate_up_scales == nullptr ||
+        down_codes == nullptr || down_scales == nullptr)
+        return CS_ERR_NULL;
+    if (plan->cfg.w_dtype != CS_MX4) return CS_ERR_UNSUPPORTED;
+    for (const cs_mx_matrix *m : {gate, up, down}) {
+        if (m->codes == nullptr || m->scales == nullptr) return CS_ERR_NULL;
+        if (!aligned(m->codes, 16) || !aligned(m->scales, 4)) return CS_ERR_UNSUPPORTED;
+    }
+    if (!aligned(gate_up_codes, 32) || !aligned(gate_up_scales, 16) || !aligned(down_codes, 32) || !aligned(down_scales, 16))
+        return CS_ERR_UNSUPPORTED;
+    const int dk = plan->cfg.d / 128, G = plan->G;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_pdl(true, pack_tiles_kernel, dim3(2 * G * dk), dim3(256), 0, st, gate->codes, gate->scales, up->codes, up->scales, dk,
+                               gate_up_codes, gate_up_scales);
+    if (e == cudaSuccess)
+        e = launch_pdl(true, pack_tiles_kernel, dim3(dk * G), dim3(256), 0, st, down->codes, down->scales, nullptr, nullptr, G, down_codes, down_scales);
+    return status_of(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,461 @@
+"""The microscaled operators on the GPU against their definitions in 64 bits (mx_reference)."""
+import ctypes
+
+import pytest
+import torch
+
+import mx_reference as R
+import paper_2604_14156_b200 as cs
+from paper_2604_14156_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(g, *shape):
+    return torch.randn(shape, generator=g, device=DEV)
+
+
+# ---- quantisation ------------------------------------------------------------------------------------
+
+def check_quantized(w, transpose):
+    codes, scales = cs.cs_mx_quantize(w, transpose=transpose)
+    m = w.t() if transpose else w
+    v, byte = R.quantize4(m)
+    assert codes.shape == (m.shape[0], 16 * byte.shape[1]) and scales.shape == byte.shape
+    assert torch.equal(scales.view(torch.uint8), byte)
+    assert torch.equal(R.codes4(codes), v)
+    back = cs.cs_mx_dequantize(codes, scales, m.shape[1], w.dtype)
+    # values are exact in both types but for 2^128, which magnitudes above 3.5 2^126 round to: an infinity
+    exact = R.values4(codes, scales)[:, :m.shape[1]]
+    want = exact.to(w.dtype).double()
+    assert torch.equal(want[exact.abs() < 2.0 ** 128], exact[exact.abs() < 2.0 ** 128])
+    assert torch.equal(torch.isnan(back), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(back.double()), torch.nan_to_num(want))
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 32), (32, 1), (3, 33), (31, 64), (129, 8), (257, 100), (64, 1000), (300, 514), (1031, 2051), (256, 64)])
+def test_quantize_matches_definition(rows, cols, dtype, transpose):
+    w = randn(gen(rows * 7 + cols), rows, cols) * torch.exp(3 * randn(gen(5), rows, 1))
+    check_quantized(w.to(dtype), transpose)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantize_extreme_values(dtype, transpose):
+    w = torch.zeros((96, 96), device=DEV)
+    w[0, 0] = float("nan")
+    w[33, 1] = float("inf")
+    w[34, 40] = -float("inf")
+    w[35] = torch.finfo(torch.float32).tiny * randn(gen(1), 96)
+    w[36] = torch.finfo(torch.bfloat16).max
+    w[37] = 2.0 ** -133 * torch.arange(96, device=DEV)
+    w[38, ::2], w[38, 1::2] = 6.0, -0.25            # a tie between 0 and 0.5: 0
+    w[39] = torch.tensor([0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, -2.5], device=DEV).repeat(12)    # ties of every binade
+    w[40] = torch.nextafter(torch.tensor(6.0), torch.tensor(7.0)).item() if dtype == torch.float32 else 6.03125
+    w[41, 3] = -0.0
+    w[70:, 70:] = 3e38
+    check_quantized(w.to(dtype), transpose)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+def test_quantize_strided_and_unaligned(transpose):
+    base = randn(gen(3), 200, 333).bfloat16()
+    for view in (base[:, 1:130], base[3:150, 8:136], base[::2, :64], base[5:6, 7:300]):
+        check_quantized(view, transpose)
+    out = torch.full((40, 100), 7.0, device=DEV)
+    codes, scales = cs.cs_mx_quantize(base[:40, :70])
+    cs.cs_mx_dequantize(codes, scales, 70, out=out[:, 10:80])
+    assert torch.equal(out[:, 10:80].double(), R.values4(codes, scales)[:, :70])
+    assert (out[:, :10] == 7).all() and (out[:, 80:] == 7).all()
+
+
+def test_quantize_refusals():
+    w = randn(gen(1), 64, 64)
+    with pytest.raises(ValueError):
+        cs.cs_mx_quantize(w.t())
+    with pytest.raises(ValueError):
+        cs.cs_mx_quantize(w[:0])
+    with pytest.raises(TypeError):
+        cs.cs_mx_quantize(w.half())
+    codes, scales = cs.cs_mx_quantize(w)
+    with pytest.raises(ValueError):
+        cs.cs_mx_dequantize(codes, scales, 65)
+    with pytest.raises(TypeError):
+        cs.cs_mx_dequantize(codes, scales.float(), 64)
+    with pytest.raises(ValueError):
+        cs.cs_mx_quantize(w, codes=codes[:, :16])
+
+
+# ---- norm ----------------------------------------------------------------------------------------------
+
+def check_norm(x, gamma, delta, eps, got, rows=None):
+    h, q, s, n = got
+    B, d = x.shape
+    want_h = x if delta is None else (x.float() + delta.float()).to(x.dtype)
+    assert torch.equal(torch.nan_to_num(h.double(), nan=1e300), torch.nan_to_num(want_h.double(), nan=1e300))
+    f = want_h.double()
+    want = f / torch.sqrt(f.square().mean(1, keepdim=True) + eps) * (1 if gamma is None else gamma.double())
+    # a row with a NaN is NaN; with an infinity, h / inf is 0 but for the infinity itself, whose block is NaN
+    fine = torch.isfinite(want).reshape(B, -1, 32).all(2).repeat_interleave(32, dim=1)
+    # h itself is exact; the sum of squares (f32, a tree) enters with half its error, then root, division and two products: 2^-20 in all
+    err = 2.0 ** -20 * want.abs()
+    if n is not None:
+        assert ((n.double() - want).abs() <= err)[fine].all() and torch.isnan(n[torch.isnan(want)]).all()
+    scale = R.untiles(s, B, d // 32)
+    value = q.double() * scale.repeat_interleave(32, dim=1)
+    assert torch.isnan(value[~fine]).all()
+    want = torch.where(fine, want, torch.zeros_like(want))
+    _, step, _ = R.round8(want)
+    # half a step of e4m3; a scale whose block's largest lies on the border may be the next one, which doubles the steps of the smallest elements
+    top = want.abs().reshape(B, d // 32, 32).amax(-1)
+    want_scale = R.two_to(R.exponent(top, 448.0))
+    lo, hi = R.two_to(R.exponent(top * (1 - 2.0 ** -20), 448.0)), R.two_to(R.exponent(top * (1 + 2.0 ** -20), 448.0))
+    good = fine[:, ::32]
+    assert ((scale >= lo) & (scale <= hi))[good].all()
+    step = torch.where((lo < hi).repeat_interleave(32, dim=1), 2 * step, step)
+    assert ((value - want).abs() <= step / 2 + 2.0 ** -20 * want.abs())[fine].all()
+    # most scales are those of the definition
+    assert (scale == want_scale)[good].double().mean() > 0.99
+    # padding of the last tile of 128 rows
+    byte = torch.zeros((B, d // 32), dtype=torch.uint8, device=x.device)
+    pad = R.tiles(byte + 1) == 0
+    assert (s.view(torch.uint8)[pad] == 0).all()
+
+
+@pytest.mark.parametrize("B,d", [(1, 128), (1, 4096), (2, 640), (33, 256), (127, 1152), (128, 384), (129, 5120), (300, 128), (5, 8192), (1025, 512)])
+@pytest.mark.parametrize("xt,dt", [(torch.float32, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32),
+                                   (torch.float32, None), (torch.bfloat16, None)])
+def test_norm_matches_definition(B, d, xt, dt):
+    g = gen(B + d)
+    x = (randn(g, B, d) * torch.exp(2 * randn(g, B, 1)) * (1 + 50 * (randn(g, 1, d) > 2.5))).to(xt)
+    delta = None if dt is None else randn(g, B, d).to(dt)
+    gamma = None if B == 2 else 1 + 0.2 * randn(g, d)
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    before = x.clone()
+    got = cs.cs_mx_norm(plan, x, gamma, delta=delta, want_n=B != 33)
+    assert torch.equal(x, before)
+    check_norm(x, gamma, delta, 1e-5, got)
+    assert plan.device_status() == 0
+    # in place: the residual stream updated where it stands
+    y = x.clone()
+    again = cs.cs_mx_norm(plan, y, gamma, delta=delta, x_out=y)
+    assert again[0] is y and torch.equal(y, got[0])
+    assert torch.equal(again[1].view(torch.uint8), got[1].view(torch.uint8)) and torch.equal(again[2].view(torch.uint8), got[2].view(torch.uint8))
+    plan.close()
+
+
+def test_norm_rows_of_zeros_nan_and_infinity():
+    g = gen(2)
+    x = randn(g, 6, 256)
+    x[1] = 0
+    x[2, 17] = float("nan")
+    x[3, 200] = float("inf")
+    x[4] = 1e-30
+    x[5, 3] = 1e15
+    plan = cs.Plan(256, 128, 128, 1, 1, 0, "mx4", 6, 1e-5)
+    got = cs.cs_mx_norm(plan, x, None, want_n=True)
+    check_norm(x, None, None, 1e-5, got)
+    assert (got[1][1].float() == 0).all()
+    plan.close()
+
+
+def test_norm_refusals():
+    plan = cs.Plan(256, 128, 128, 1, 1, 0, "mx4", 4, 1e-5)
+    x = randn(gen(1), 4, 256)
+    with pytest.raises(TypeError):
+        cs.cs_mx_norm(plan, x.half())
+    with pytest.raises(ValueError):
+        cs.cs_mx_norm(plan, x[:, :128])
+    with pytest.raises(ValueError):
+        cs.cs_mx_norm(plan, x, delta=x[:2])
+    with pytest.raises(TypeError):
+        cs.cs_mx_norm(plan, x.cpu())
+    with pytest.raises(cs.CSError) as e:
+        cs.cs_mx_norm(plan, torch.zeros((5, 256), device=DEV))
+    assert e.value.code == 2
+    with pytest.raises(cs.CSError) as e:
+        cs.cs_mx_norm(plan, torch.zeros(4 * 256 + 1, device=DEV)[1:].view(4, 256))
+    assert e.value.code == 3
+    other = cs.Plan(256, 128, 128, 1, 1, 0, torch.bfloat16, 4, 1e-5)
+    with pytest.raises(cs.CSError) as e:
+        cs.cs_mx_norm(other, x)
+    assert e.value.code == 3
+    plan.close()
+    other.close()
+
+
+# ---- FFN -------------------------------------------------------------------------------------------------
+
+class Problem:
+    def __init__(self, B, d, G, k, shared, seed=0, plan_tokens=None):
+        g = gen(1000 * seed + B + d + G)
+        self.B, self.d, self.G, self.k, self.shared = B, d, G, k, shared
+        d_ff = 128 * G
+        self.gate, self.up = (cs.cs_mx_quantize(randn(g, d_ff, d) / d ** 0.5) for _ in range(2))
+        self.down = cs.cs_mx_quantize((randn(g, d_ff, d) / (128 * k) ** 0.5).bfloat16(), transpose=True)
+        self.plan = cs.Plan(d, d_ff, 128, 1, k, 0, "mx4", plan_tokens or B, 1e-5)
+        self.layer = cs.MxLayer(self.plan, self.gate, self.up, self.down)
+        self.new_inputs(g, B)
+
+    def new_inputs(self, g, B):
+        self.B = B
+        x = randn(g, B, self.d) * torch.exp(randn(g, B, 1))
+        _, self.q, self.s, _ = cs.cs_mx_norm(self.plan, x)
+        # rows differ in size: the norm has evened them out, so scale some blocks' bytes
+        draw = torch.rand((1 if self.shared else B, self.G), generator=g, device=DEV)
+        sup = draw.topk(self.k, dim=1).indices.sort(dim=1).values.to(torch.int32)
+        self.support = sup[0].contiguous() if self.shared else sup
+
+    def run(self, **kw):
+        return (cs.cs_mx_ffn_shared if self.shared else cs.cs_mx_ffn)(self.plan, self.layer, self.q, self.s, self.support, **kw)
+
+    def operands(self):
+        x = self.q.double() * R.untiles(self.s, self.B, self.d // 32).repeat_interleave(32, dim=1)
+        return x, R.values4(*self.gate), R.values4(*self.up), R.values4(*self.down)
+
+    def member(self):
+        m = torch.zeros((self.support.reshape(-1, self.k).shape[0], self.G), dtype=torch.bool, device=DEV)
+        m.scatter_(1, self.support.reshape(-1, self.k).long(), True)
+        return m.expand(self.B, self.G).repeat_interleave(128, dim=1)
+
+    def check(self, out):
+        want, tol = R.ffn(*self.operands(), self.member())
+        off = (out.double() - want).abs()
+        assert (off <= tol).all(), float((off / tol).max())
+        assert self.plan.device_status() == 0
+
+
+TOKENS = [1, 2, 3, 15, 16, 17, 31, 33, 64, 65, 100, 112, 113, 127, 128, 129, 144, 200, 255, 256, 257, 300, 513]
+
+
+@pytest.mark.parametrize("B", TOKENS)
+def test_ffn_every_batch(B):
+    p = Problem(B, 512, 12, 5, False)
+    p.check(p.run())
+    p.plan.close()
+
+
+@pytest.mark.parametrize("n", TOKENS + [777, 1025])
+def test_ffn_shared_every_length(n):
+    p = Problem(n, 384, 9, 4, True)
+    p.check(p.run())
+    p.plan.close()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("d,G,k", [(128, 1, 1), (128, 128, 128), (256, 2, 1), (640, 7, 7), (1152, 3, 2), (4096, 86, 22), (8192, 4, 3), (5120, 20, 11), (1280, 128, 1)])
+def test_ffn_shapes(d, G, k, shared):
+    for B in (1, 5, 64, 140):
+        p = Problem(B, d, G, k, shared, seed=3)
+        p.check(p.run())
+        p.plan.close()
+
+
+def test_ffn_rows_behind_the_batch_stay_and_scratch_is_reused():
+    """Batches of every size through one plan, larger ones first; the output's other rows keep what they held."""
+    p = Problem(300, 256, 10, 3, False)
+    g = gen(9)
+    for B in (300, 7, 129, 1, 40):
+        p.new_inputs(g, B)
+        out = torch.full((320, p.d), 3.0, dtype=torch.bfloat16, device=DEV)
+        p.run(out=out[:B])
+        p.check(out[:B])
+        assert (out[B:] == 3).all()
+    p.plan.close()
+
+
+def test_ffn_scales_of_padding_rows_may_be_anything():
+    p = Problem(20, 256, 6, 2, False)
+    want = p.run()
+    raw = p.s.view(torch.uint8)
+    pad = R.tiles(torch.ones((20, 8), dtype=torch.uint8, device=DEV)) == 0
+    raw[pad] = 255
+    assert torch.equal(p.run(), want)
+    p.check(want)
+    p.plan.close()
+
+
+def test_ffn_a_row_of_nan_keeps_to_itself():
+    p = Problem(70, 256, 6, 2, False)
+    want = p.run()
+    q = p.q.view(torch.uint8)
+    q[3, 17] = 0x7F
+    p.s.view(torch.uint8)[0, 1, 40 % 32, 40 // 32, 2] = 255     # row 40, block 6
+    got = p.run()
+    bad = torch.zeros(70, dtype=torch.bool, device=DEV)
+    bad[3] = bad[40] = True
+    assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], want[~bad])
+    p.plan.close()
+
+
+@pytest.mark.parametrize("B", [1, 6, 40])
+def test_ffn_invalid_supports_count_for_nothing_and_are_reported(B):
+    p = Problem(B, 256, 6, 3, False)
+    p.support[0] = torch.tensor([-1, 2, 6], dtype=torch.int32)
+    out = p.run()
+    assert p.plan.device_status() == 4
+    m = p.member_of = torch.zeros((B, p.G), dtype=torch.bool, device=DEV)
+    m.scatter_(1, p.support.clamp(0, 5).long(), True)
+    m[0] = False
+    m[0, 2] = True
+    want, tol = R.ffn(*p.operands(), m.repeat_interleave(128, dim=1))
+    assert ((out.double() - want).abs() <= tol).all()
+    p.support[:] = -5
+    assert (p.run() == 0).all() and p.plan.device_status() == 4
+    p.support[:] = 1 << 30
+    assert (p.run() == 0).all() and p.plan.device_status() == 4
+    p.support[:] = torch.tensor([1, 1, 4], dtype=torch.int32)       # a group twice: once
+    out = p.run()
+    assert p.plan.device_status() == 4
+    m[:] = False
+    m[:, 1] = m[:, 4] = True
+    want, tol = R.ffn(*p.operands(), m.repeat_interleave(128, dim=1))
+    assert ((out.double() - want).abs() <= tol).all()
+    p.plan.close()
+
+
+def test_ffn_shared_equals_own_supports_that_are_all_the_same():
+    p = Problem(50, 512, 8, 3, True)
+    own = cs.cs_mx_ffn(p.plan, p.layer, p.q, p.s, p.support.expand(50, 3).contiguous())
+    assert torch.equal(p.run(), own)
+    p.plan.close()
+
+
+def test_ffn_is_deterministic_and_rows_do_not_depend_on_their_neighbours():
+    p = Problem(64, 1024, 16, 5, False)
+    out = p.run()
+    for _ in range(3):
+        assert torch.equal(p.run(), out)
+    p.plan.close()
+
+
+def test_ffn_captured_replayed_and_on_two_streams():
+    p = Problem(37, 512, 12, 5, False)
+    eager = p.run()
+    out = torch.zeros_like(eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run(out=out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, eager)
+    g = gen(77)
+    x = randn(g, 37, 512)
+    _, q, s, _ = cs.cs_mx_norm(p.plan, x)
+    p.q.view(torch.uint8).copy_(q.view(torch.uint8))
+    p.s.view(torch.uint8).copy_(s.view(torch.uint8))
+    graph.replay()
+    torch.cuda.synchronize()
+    p.check(out)
+    # two plans, one stream each
+    a, b = Problem(5, 512, 12, 5, False, seed=1), Problem(140, 512, 12, 5, False, seed=2)
+    torch.cuda.synchronize()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(20):
+        with torch.cuda.stream(sa):
+            oa = a.run()
+        with torch.cuda.stream(sb):
+            ob = b.run()
+        outs.append((oa, ob))
+    torch.cuda.synchronize()
+    a.check(outs[0][0])
+    b.check(outs[0][1])
+    assert all(torch.equal(oa, outs[0][0]) and torch.equal(ob, outs[0][1]) for oa, ob in outs)
+    for x in (p, a, b):
+        x.plan.close()
+
+
+def test_ffn_refusals():
+    p = Problem(8, 256, 4, 2, False)
+    with pytest.raises(ValueError):
+        p.run(out=torch.zeros((7, 256), dtype=torch.bfloat16, device=DEV))
+    with pytest.raises(TypeError):
+        p.run(out=torch.zeros((8, 256), device=DEV))
+    with pytest.raises(ValueError):
+        cs.cs_mx_ffn(p.plan, p.layer, p.q, p.s, p.support[:, :1].contiguous())
+    with pytest.raises(TypeError):
+        cs.cs_mx_ffn(p.plan, p.layer, p.q.float(), p.s, p.support)
+    with pytest.raises(ValueError):
+        cs.cs_mx_ffn(p.plan, p.layer, p.q, p.s.view(-1), p.support)
+    with pytest.raises(ValueError):
+        cs.MxLayer(p.plan, p.gate, p.up, p.gate)
+    big = torch.zeros((9, 256), dtype=torch.float8_e4m3fn, device=DEV)
+    with pytest.raises(cs.CSError) as e:
+        cs.cs_mx_ffn(p.plan, p.layer, big, p.s, torch.zeros((9, 2), dtype=torch.int32, device=DEV))
+    assert e.value.code == 2
+    lib, layer = p.plan.lib, p.layer
+    args = [layer.ref, p.q.data_ptr(), p.s.data_ptr(), p.support.data_ptr(), 8, torch.zeros((8, 256), dtype=torch.bfloat16, device=DEV).data_ptr(), None]
+    for i in (1, 2, 3, 5):
+        broken = list(args)
+        broken[i] = None
+        assert lib.cs_mx_ffn(p.plan.handle, *broken) == 1
+    for i in (1, 2, 5):
+        broken = list(args)
+        broken[i] += 8
+        assert lib.cs_mx_ffn(p.plan.handle, *broken) == 3
+    bad = binding._MxLayer(layer.c.gate_up_codes + 16, layer.c.gate_up_scales, layer.c.down_codes, layer.c.down_scales)
+    assert lib.cs_mx_ffn(p.plan.handle, ctypes.byref(bad), *args[1:]) == 3
+    # a plan of one kind does not take the other kind's calls
+    other = cs.Plan(256, 512, 128, 1, 2, 0, torch.bfloat16, 8, 1e-5)
+    assert lib.cs_mx_ffn(other.handle, *args) == 3
+    w = torch.zeros((512, 256), dtype=torch.bfloat16, device=DEV)
+    plain = cs.Layer(other, torch.zeros((1, 256), device=DEV), torch.zeros((1, 4), device=DEV), w, w, w, 1.0)
+    h = torch.zeros((8, 256), device=DEV)
+    calls = [lambda: cs.cs_ffn_exec(p.plan, plain, h, p.support), lambda: cs.cs_layer_step(p.plan, plain, h),
+             lambda: cs.cs_layer_step_ex(p.plan, plain, h, cs.StepOptions(p.plan, 8)),
+             lambda: cs.cs_layer_step_host(p.plan, plain, h.cpu(), h.cpu()),
+             lambda: cs.cs_layer_step_fallback(p.plan, p.plan, plain, h, 0.5),
+             lambda: cs.cs_ffn_exec_shared(p.plan, plain, h.bfloat16(), p.support[0].contiguous()), lambda: p.plan.set_speculative(1)]
+    for call in calls:
+        with pytest.raises(cs.CSError) as e:
+            call()
+        assert e.value.code == 3
+    p.plan.close()
+    other.close()
+
+
+# ---- together -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B", [1, 9, 48])
+def test_two_layers_of_a_decode_step(B, oracle):
+    """norm -> sketch -> recovery -> FFN -> the next layer's norm, each stage against its definition on what the stage before really gave."""
+    import numpy as np
+    d, G, m, k, T = 512, 16, 16, 5, 12
+    g = gen(B)
+    plan = cs.Plan(d, 128 * G, 128, m, k, T, "mx4", B, 1e-5)
+    x, delta = randn(g, B, d), None
+    for _ in range(2):
+        gate, up = (cs.cs_mx_quantize(randn(g, 128 * G, d) / d ** 0.5) for _ in range(2))
+        down = cs.cs_mx_quantize(randn(g, 128 * G, d) / (128 * k) ** 0.5, transpose=True)
+        layer = cs.MxLayer(plan, gate, up, down)
+        S, Phi, gamma = randn(g, m, d) / d ** 0.5, randn(g, m, G) / m ** 0.5, 1 + 0.1 * randn(g, d)
+        mu = float(1 / torch.linalg.matrix_norm(Phi.double(), 2) ** 2)
+        torch.cuda.synchronize()
+        before = x.clone()
+        x, q, s, n = cs.cs_mx_norm(plan, x, gamma, delta=delta, want_n=True, x_out=x)
+        y = cs.cs_sketch(plan, S, n)
+        support, z, resid = cs.cs_recover(plan, Phi, mu, y)
+        out = cs.cs_mx_ffn(plan, layer, q, s, support)
+        assert plan.device_status() == 0
+        check_norm(before, gamma, delta, 1e-5, (x, q, s, n))
+        # f32 sums of d products
+        assert ((y.double() - n.double() @ S.double().t()).abs() <= 2.0 ** -18 * (n.double().abs() @ S.double().abs().t())).all()
+        for t in range(B):
+            ref = oracle.iht(Phi.cpu(), y[t].cpu(), k, T, mu)
+            assert np.array_equal(support[t].cpu().numpy(), ref.support) or ref.min_gap <= 1e-4
+        member = torch.zeros((B, G), dtype=torch.bool, device=DEV).scatter_(1, support.long(), True).repeat_interleave(128, dim=1)
+        xq = q.double() * R.untiles(s, B, d // 32).repeat_interleave(32, dim=1)
+        want, tol = R.ffn(xq, R.values4(*gate), R.values4(*up), R.values4(*down), member)
+        assert ((out.double() - want).abs() <= tol).all()
+        delta = out
+    plan.close()
