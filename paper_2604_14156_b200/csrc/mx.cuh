@@ -51,10 +51,11 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
         "mov.b32 %0, {lo, hi};\n}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
     return r;
 }
-__device__ __forceinline__ uint8_t to_e4m3(float a) {
+// Two floats as e4m3 bytes, the first in the lower.
+__device__ __forceinline__ uint16_t pack_e4m3x2(float a, float b) {
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(a));
-    return (uint8_t)r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+    return r;
 }
 
 // mx_norm.cu
@@ -62,6 +63,7 @@ cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *
                          void *x_out, float *n_out, uint8_t *q, uint8_t *s, cudaStream_t st);
 // mx_ffn.cu: support [B, k], or with `shared` [k]
 cs_status prepare_mx_ffn(cs_plan *plan);
+size_t mx_wide_partial_bytes(const cs_plan *plan);   // mx_wide.cu's scratch for parts of an output
 cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const uint8_t *s, const int32_t *support, bool shared,
                         int B, void *out, cudaStream_t st);
 

@@ -1,0 +1,76 @@
+// What the FFN kernels on microscaled operands share (mx_ffn.cu: batches whose tokens fit the N side of one instruction; mx_wide.cu: larger ones).
+#pragma once
+
+#include "mma_core.cuh"
+#include "mx.cuh"
+
+namespace cs {
+
+// What a launch needs to know beside its tensor maps.
+struct MxArgs {
+    const uint8_t *w_scales, *x_scales;
+    const int32_t *support;         // fold: [B, k] or, without mask, [k]
+    int32_t *list, *count;          // groups of the union, ascending
+    unsigned *ready;                // set while a call's list stands, before its gate/up is complete
+    const uint32_t *mask;           // [B, 4] membership bits, unless folded
+    uint8_t *a, *a_scales;          // gate/up's result
+    __nv_bfloat16 *out;             // down's
+    DeviceStatus *status;
+    int B, d, G, k;
+    int cap;                        // groups the list can hold: pitch of a and its scales
+    int tile, stages;               // tokens of a tile, ring stages
+    int shared, fold;               // one support for all tokens; gate/up makes the list
+    int w_once;                     // weights are read by one token tile only
+};
+
+// A batch on CTA pairs (mx_wide.cu); the list stands in p.list unless p.fold.
+cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const MxArgs &p, cudaStream_t st);
+cs_status prepare_mx_wide(cs_plan *plan);
+
+namespace {
+
+constexpr int kMxWBytes = 128 * 128;                 // a weight tile in shared memory
+constexpr int kMxWLoad = 128 * 64;                   // ... and in memory, which is what the barrier counts
+// Ring position without divisions: the issue of a k block's copies is what a CTA's weight stream waits for first.
+struct MxRing {
+    int stage = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++stage == stages) { stage = 0; phase ^= 1; }
+    }
+};
+__device__ __forceinline__ bool mx_wait(uint64_t *bar, uint32_t parity, uint32_t *aborted, DeviceStatus *status) {
+    const uint32_t addr = smem_u32(bar);
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+        if (done) return true;
+        if (*reinterpret_cast<volatile uint32_t *>(aborted)) return false;
+    }
+    *reinterpret_cast<volatile uint32_t *>(aborted) = 1;
+    atomicCAS(&status->code, 0, (int)CS_ERR_TIMEOUT);
+    return false;
+}
+// Matrix of bytes [rows, inner]: boxes of 128 bytes x box_rows, 128-byte swizzle.
+bool make_map_bytes(CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows, uint32_t box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {inner};
+    const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Packed weight tiles, seen as rows of 128 four-bit elements: a box is a tile, or some rows of one.
+bool make_map_tiles(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_rows = 128) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {128, tiles * 128}, strides[1] = {64};
+    const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+}  // namespace cs

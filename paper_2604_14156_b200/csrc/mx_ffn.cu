@@ -15,38 +15,26 @@
 // accumulators are added over distributed shared memory in a fixed order.
 #include <stdio.h>
 
-#include "mma_core.cuh"
-#include "mx.cuh"
+#include "mx_core.cuh"
 
 namespace cs {
 
 namespace {
 
 constexpr int kMxEpiWarps = 8;
-constexpr int kMxThreads = 64 + 32 * kMxEpiWarps;    // TMA warp, MMA warp, epilogue
+constexpr int kMxThreads = 128 + 32 * kMxEpiWarps;   // weight loads, MMA, token loads, one idle warp; epilogue
 constexpr int kMxMaxTile = 256;                      // tokens of a tile
 constexpr int kMxMaxStages = 8;
-constexpr int kMxWBytes = 128 * 128;                 // a weight tile in shared memory
-constexpr int kMxWLoad = 128 * 64;                   // ... and in memory, which is what the barrier counts
 constexpr int kMxMaxCluster = 8;
-
-// What a launch needs to know beside its tensor maps.
-struct MxArgs {
-    const uint8_t *w_scales, *x_scales;
-    const int32_t *list, *count;    // groups of the union, ascending
-    const uint32_t *mask;           // [B, 4] membership bits, or NULL: every token uses every listed group
-    uint8_t *a, *a_scales;          // gate/up's result
-    __nv_bfloat16 *out;             // down's
-    DeviceStatus *status;
-    int B, d, G;
-    int cap;                        // groups the list can hold: pitch of a and its scales
-    int tile, stages;               // tokens of a tile, ring stages
-    int w_once;                     // weights are read by one token tile only
-};
+constexpr int kMxNarrowTokens = 128;                 // larger batches take the pairs of mx_wide.cu
+constexpr int kMxFoldEntries = 2048;                 // up to this many support entries gate/up makes the list itself
 
 struct MxBars {
     uint64_t full[kMxMaxStages], empty[kMxMaxStages], acc;
     uint32_t tmem, aborted;
+    uint32_t all[4];                // the union
+    int32_t list[kMaxG], count;
+    uint32_t bits[kMxMaxTile / 32]; // fold: which tokens of the tile use this CTA's group
 };
 
 __host__ __device__ inline int mx_chunks(int tile) { return (tile + 127) / 128; }
@@ -60,19 +48,6 @@ __host__ __device__ inline int mx_tmem_cols(int tile, int stages) {
     return c;
 }
 
-__device__ __forceinline__ bool mx_wait(uint64_t *bar, uint32_t parity, MxBars *b, DeviceStatus *status) {
-    const uint32_t addr = smem_u32(bar);
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
-        uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
-        if (done) return true;
-        if (*reinterpret_cast<volatile uint32_t *>(&b->aborted)) return false;
-    }
-    b->aborted = 1;
-    atomicCAS(&status->code, 0, (int)CS_ERR_TIMEOUT);
-    return false;
-}
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
@@ -92,15 +67,29 @@ __device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t a, uint64_t b, ui
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
 }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kMxEpiWarps) : "memory"); }
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
+}
+
+__device__ __forceinline__ void mx_list_of(const uint32_t (&all)[4], int32_t *list, int32_t *count) {
+    if (threadIdx.x < 128) {
+        const int g = threadIdx.x, w = g >> 5;
+        int before = 0, n = 0;
+        for (int i = 0; i < 4; ++i) {
+            if (i < w) before += __popc(all[i]);
+            n += __popc(all[i]);
+        }
+        before += __popc(all[w] & ((1u << (g & 31)) - 1));
+        if (all[w] >> (g & 31) & 1) list[before] = g;
+        if (g == 0) *count = n;
+    }
 }
 
 // One CTA: the union of all rows of `support`, the rows' membership bits (when mask != NULL), validation.  A thread per entry, so that all loads
@@ -144,92 +133,123 @@ mx_list_kernel(const int32_t *support, int rows, int k, int G, uint32_t *mask, i
         __syncthreads();
     }
     if (bad) atomicCAS(&status->code, 0, (int)CS_ERR_SUPPORT);
-    if (threadIdx.x < 128) {
-        const int g = threadIdx.x, w = g >> 5;
-        int before = 0, n = 0;
-        for (int i = 0; i < 4; ++i) {
-            if (i < w) before += __popc(all[i]);
-            n += __popc(all[i]);
-        }
-        before += __popc(all[w] & ((1u << (g & 31)) - 1));
-        if (all[w] >> (g & 31) & 1) list[before] = g;
-        if (g == 0) *count = n;
-    }
+    mx_list_of(all, list, count);
 }
 
-// The part both products share: accumulators of this CTA's k blocks [first, first + n) of weight tile row `wrow` (in tiles: the first k
-// block's index in the packed matrix; listed: k block j is list[j]) against token tile `z`.  Leaves the accumulators in the shared tile
-// [columns][128], zeros where there was no k block.
+// The union of `rows` rows of supports into bars->all, by all threads; `mine` (or -1): bars->bits says which rows hold that group.
+__device__ __forceinline__ void mx_union(const int32_t *support, int rows, int k, int G, MxBars *bars, int mine, DeviceStatus *status) {
+    for (int i = threadIdx.x; i < 4 + kMxMaxTile / 32; i += kMxThreads) (i < 4 ? bars->all[i] : bars->bits[i - 4]) = 0;
+    __syncthreads();
+    const int n = rows * k;
+    bool bad = false;
+    constexpr int kAhead = (kMxFoldEntries + kMxThreads - 1) / kMxThreads;
+    int g[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int i = threadIdx.x + u * kMxThreads;
+        g[u] = i < n ? ld_dep(support + i) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int i = threadIdx.x + u * kMxThreads;
+        if (i < n) {
+            if (status != nullptr) bad |= g[u] >= G || g[u] <= (i % k != 0 ? ld_dep(support + i - 1) : -1);
+            if (g[u] >= 0 && g[u] < G) {
+                const uint32_t bit = 1u << (g[u] & 31);
+                if (!(*reinterpret_cast<volatile uint32_t *>(&bars->all[g[u] >> 5]) & bit)) atomicOr(&bars->all[g[u] >> 5], bit);
+            }
+        }
+    }
+    if (bad) atomicCAS(&status->code, 0, (int)CS_ERR_SUPPORT);
+    __syncthreads();
+}
 struct MxRange { int first, n; };
 
+// Three warps feed and run the products of k blocks [r.first, r.first + r.n) against token tile z.  Weight tile of k block j: wtile + j, or with DOWN
+// wtile + list[j].
 template <bool DOWN>
-__device__ __forceinline__ void mx_mainloop(const CUtensorMap *wmap, const CUtensorMap *xmap, const MxArgs &p, uint8_t *smem, MxBars *bars, int64_t wtile,
-                                            MxRange r, int z, int columns) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ void mx_load_weights(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, int wtile, MxRange r) {
+    const uint64_t policy = policy_evict_first();
+    const int stage_bytes = mx_stage_bytes(p.tile), scales = kMxWBytes + p.tile * 128;
+    MxRing ring;
+    for (int i = 0; i < r.n; ++i) {
+        if (i >= p.stages && !mx_wait(&bars->empty[ring.stage], ring.phase ^ 1, &bars->aborted, p.status)) return;
+        uint8_t *w = smem + ring.stage * stage_bytes;
+        uint64_t *full = &bars->full[ring.stage];
+        const int tile = wtile + (DOWN ? bars->list[r.first + i] : r.first + i);
+        mbar_expect_tx(full, kMxWLoad + kMxTileBytes);
+        if (p.w_once) tma_load_2d(w, map, 0, tile * 128, full, policy);
+        else tma_load_2d(w, map, 0, tile * 128, full);
+        bulk_load(w + scales, p.w_scales + (size_t)tile * kMxTileBytes, kMxTileBytes, full);
+        ring.next(p.stages);
+    }
+}
+__device__ __forceinline__ void mx_load_tokens(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int z, int kpitch) {
     const int stage_bytes = mx_stage_bytes(p.tile), chunks = mx_chunks(p.tile);
-    const int kpitch = DOWN ? p.cap : p.d >> 7;          // k blocks of the token operand
-    if (warp == 0) {
-        if (lane == 0) {
-            const uint64_t policy = policy_evict_first();
-            const uint32_t bytes = kMxWLoad + p.tile * 128 + kMxTileBytes * (1 + chunks);
-            const int last_chunk = (p.B - 1) >> 7;
-            for (int i = 0; i < r.n; ++i) {
-                const int s = i % p.stages, j = r.first + i;
-                if (i >= p.stages && !mx_wait(&bars->empty[s], (i / p.stages - 1) & 1, bars, p.status)) break;
-                uint8_t *w = smem + (size_t)s * stage_bytes, *x = w + kMxWBytes, *sc = x + p.tile * 128;
-                const int64_t tile = wtile + (DOWN ? ld_dep(p.list + j) : j);
-                mbar_expect_tx(&bars->full[s], bytes);
-                if (p.w_once) tma_load_2d(w, wmap, 0, (int)(tile * 128), &bars->full[s], policy);
-                else tma_load_2d(w, wmap, 0, (int)(tile * 128), &bars->full[s]);
-                tma_load_2d(x, xmap, j * 128, z * p.tile, &bars->full[s]);
-                bulk_load(sc, p.w_scales + tile * kMxTileBytes, kMxTileBytes, &bars->full[s]);
-                for (int c = 0; c < chunks; ++c)      // behind the last row: any tile that exists
-                    bulk_load(sc + kMxTileBytes * (1 + c), p.x_scales + ((size_t)min(z * p.tile / 128 + c, last_chunk) * kpitch + j) * kMxTileBytes,
-                              kMxTileBytes, &bars->full[s]);
-            }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t scales = bars->tmem + p.tile;
-            for (int i = 0; i < r.n; ++i) {
-                const int s = i % p.stages;
-                if (!mx_wait(&bars->full[s], (i / p.stages) & 1, bars, p.status)) break;
-                tc_fence_after();
-                const uint32_t w = smem_u32(smem + (size_t)s * stage_bytes), x = w + kMxWBytes, sc = x + p.tile * 128;
-                const uint32_t sa = scales + s * 4 * (1 + chunks), sb = sa + 4;
-                tc_copy_scales(sa, sc);
-                for (int c = 0; c < chunks; ++c) tc_copy_scales(sb + 4 * c, sc + kMxTileBytes * (1 + c));
-                const uint64_t ad = desc_sw128(w, 0), bd = desc_sw128(x, 0);
+    // behind the last row: any tile of scales that exists
+    const uint8_t *s0 = p.x_scales + (size_t)min(z * p.tile >> 7, (p.B - 1) >> 7) * kpitch * kMxTileBytes;
+    const uint8_t *s1 = p.x_scales + (size_t)min((z * p.tile >> 7) + 1, (p.B - 1) >> 7) * kpitch * kMxTileBytes;
+    MxRing ring;
+    for (int i = 0; i < r.n; ++i) {
+        if (i >= p.stages && !mx_wait(&bars->empty[ring.stage], ring.phase ^ 1, &bars->aborted, p.status)) return;
+        uint8_t *x = smem + ring.stage * stage_bytes + kMxWBytes;
+        uint64_t *full = &bars->full[ring.stage];
+        const int j = r.first + i;
+        mbar_expect_tx(full, p.tile * 128 + kMxTileBytes * chunks);
+        tma_load_2d(x, map, j * 128, z * p.tile, full);
+        uint8_t *sc = x + p.tile * 128 + kMxTileBytes;
+        bulk_load(sc, s0 + (size_t)j * kMxTileBytes, kMxTileBytes, full);
+        if (chunks > 1) bulk_load(sc + kMxTileBytes, s1 + (size_t)j * kMxTileBytes, kMxTileBytes, full);
+        ring.next(p.stages);
+    }
+}
+__device__ __forceinline__ void mx_products(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int columns) {
+    const int stage_bytes = mx_stage_bytes(p.tile), chunks = mx_chunks(p.tile);
+    uint32_t idesc[4];
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) tc_mma_mx(bars->tmem, ad + 2 * kk, bd + 2 * kk, mx_idesc(columns, kk), sa, sb, (i | kk) != 0);
-                tc_commit(&bars->empty[s]);
-            }
-            if (r.n > 0) tc_commit(&bars->acc);
-        }
-        __syncwarp();
-    } else {
-        const int e = warp - 2, quarter = warp & 3, half = e >> 2;
-        float *tile = reinterpret_cast<float *>(smem);
-        const bool ok = r.n > 0 && mx_wait(&bars->acc, 0, bars, p.status);
+    for (int kk = 0; kk < 4; ++kk) idesc[kk] = mx_idesc(columns, kk);
+    const uint32_t base = smem_u32(smem), tmem = bars->tmem;
+    MxRing ring;
+    for (int i = 0; i < r.n; ++i) {
+        if (!mx_wait(&bars->full[ring.stage], ring.phase, &bars->aborted, p.status)) break;
         tc_fence_after();
-        // the ring is drained: the tile takes its place
-        for (int c = 16 * half; c < columns; c += 32) {
-            uint32_t v[16];
-            if (ok) { tc_ld16(bars->tmem + ((uint32_t)quarter << 21) + c, v); tc_wait_ld(); }
+        const uint32_t w = base + ring.stage * stage_bytes, x = w + kMxWBytes, sc = x + p.tile * 128;
+        const uint32_t sa = tmem + p.tile + ring.stage * 4 * (1 + chunks), sb = sa + 4;
+        tc_copy_scales(sa, sc);
+        tc_copy_scales(sb, sc + kMxTileBytes);
+        if (chunks > 1) tc_copy_scales(sb + 4, sc + 2 * kMxTileBytes);
+        const uint64_t ad = desc_sw128(w, 0), bd = desc_sw128(x, 0);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) tile[(c + j) * 128 + quarter * 32 + lane] = ok ? __uint_as_float(v[j]) : 0.f;
-        }
+        for (int kk = 0; kk < 4; ++kk) tc_mma_mx(tmem, ad + 2 * kk, bd + 2 * kk, idesc[kk], sa, sb, (i | kk) != 0);
+        tc_commit(&bars->empty[ring.stage]);
+        ring.next(p.stages);
+    }
+    if (r.n > 0) tc_commit(&bars->acc);
+}
+// The accumulators of the tile's valid tokens to shared memory, [column][128 rows], over the drained ring; zeros where there was no k block.
+__device__ __forceinline__ void mx_spill(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int valid) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
+    float *tile = reinterpret_cast<float *>(smem) + quarter * 32 + lane;
+    const bool ok = r.n > 0 && mx_wait(&bars->acc, 0, &bars->aborted, p.status);
+    tc_fence_after();
+    for (int c = 16 * ((warp >> 2) - 1); c < valid; c += 32) {
+        uint32_t v[16];
+        if (ok) { tc_ld16(bars->tmem + ((uint32_t)quarter << 21) + c, v); tc_wait_ld(); }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < valid) tile[(c + j) * 128] = ok ? __uint_as_float(v[j]) : 0.f;
     }
 }
 
-__device__ __forceinline__ uint8_t *mx_setup(MxBars *bars, int stages, int cols) {
+__device__ __forceinline__ uint8_t *mx_setup(MxBars *bars, int stages, int cols, const CUtensorMap *a, const CUtensorMap *b) {
     extern __shared__ uint8_t raw[];
     if (threadIdx.x == 0) {
-        for (int s = 0; s < stages; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(&bars->full[s], 2); mbar_init(&bars->empty[s], 1); }
         mbar_init(&bars->acc, 1);
         bars->aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(b) : "memory");
     }
     if (threadIdx.x >> 5 == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(cols) : "memory");
@@ -254,42 +274,76 @@ __global__ void __launch_bounds__(kMxThreads)
 mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const MxArgs p) {
     __shared__ MxBars bars;
     const int cs = gridDim.x, rank = blockIdx.x, entry = blockIdx.y >> 1, half = blockIdx.y & 1, z = blockIdx.z;
-    const int kb = p.d >> 7, cols = mx_tmem_cols(p.tile, p.stages);
-    uint8_t *smem = mx_setup(&bars, p.stages, cols);
+    const int kb = p.d >> 7, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *smem = mx_setup(&bars, p.stages, cols, &wmap, &xmap);
     pdl_wait();
     pdl_launch_dependents();
-    if (entry < ld_dep(p.count)) {      // the same in every CTA of a cluster
-        const int g = ld_dep(p.list + entry);
-        const int columns = min(p.tile, (p.B - z * p.tile + 15) & ~15);
+    const bool first = blockIdx.x + blockIdx.y + blockIdx.z == 0;
+    if (p.fold) {
+        mx_union(p.support, p.shared ? 1 : p.B, p.k, p.G, &bars, -1, first ? p.status : nullptr);
+        mx_list_of(bars.all, bars.list, &bars.count);
+        __syncthreads();
+        if (first) {      // for the down product, which may read it once `ready` is set
+            if ((int)threadIdx.x < bars.count) p.list[threadIdx.x] = bars.list[threadIdx.x];
+            if (threadIdx.x == 0) *p.count = bars.count;
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
+        }
+    } else {
+        if (threadIdx.x == 0) { bars.count = ld_dep(p.count); bars.list[entry] = ld_dep(p.list + entry); }
+        __syncthreads();
+        if (first && threadIdx.x == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
+    }
+    if (entry < bars.count) {      // the same in every CTA of a cluster
+        const int g = bars.list[entry];
+        const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
         const MxRange r = {kb * rank / cs, kb * (rank + 1) / cs - kb * rank / cs};
-        mx_mainloop<false>(&wmap, &xmap, p, smem, &bars, (int64_t)(2 * g + half) * kb, r, z, columns);
+        if (warp == 0) {
+            if (lane == 0) mx_load_weights<false>(&wmap, p, smem, &bars, (2 * g + half) * kb, r);
+        } else if (warp == 1) {
+            if (lane == 0) mx_products(p, smem, &bars, r, columns);
+        } else if (warp == 2) {
+            if (lane == 0) mx_load_tokens(&xmap, p, smem, &bars, r, z, kb);
+        } else if (warp >= 4) {
+            if (p.fold && !p.shared)      // while the products run: who uses this group
+                for (int t = threadIdx.x - 128; t < valid * p.k; t += 32 * kMxEpiWarps)
+                    if (ld_dep(p.support + (size_t)z * p.tile * p.k + t) == g) atomicOr(&bars.bits[t / p.k >> 5], 1u << (t / p.k & 31));
+            mx_spill(p, smem, &bars, r, valid);
+        }
+        __syncwarp();
         if (cs > 1) cluster_sync_all();
-        const int e = (int)(threadIdx.x >> 5) - 2, lane = threadIdx.x & 31;
-        if (e >= 0) {
+        if (warp >= 4) {
             if (cs == 1) epilogue_sync();
-            // (column, block of 32 channels) pairs, a warp each: a lane is a channel
-            const uint32_t base = smem_u32(smem);
-            for (int i = e; (i >> 1) * cs < columns; i += kMxEpiWarps) {
-                const int c = (i >> 1) * cs + rank, b = i & 1, t = z * p.tile + c;
-                if (c >= columns || t >= p.B) continue;
-                float gate = 0.f, up = 0.f;
-                const uint32_t at = base + (uint32_t)(c * 128 + b * 32 + lane) * 4;
+            // a column to a warp, two neighbouring channels to a lane: lanes 0..15 hold one block of 32, lanes 16..31 the other
+            const uint32_t base = smem_u32(smem) + lane * 8;
+#pragma unroll 2
+            for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
+                const int t = z * p.tile + c;
+                float g0 = 0.f, g1 = 0.f, u0 = 0.f, u1 = 0.f;
                 if (cs == 1) {
-                    const float *tile = reinterpret_cast<const float *>(smem) + c * 128 + b * 32 + lane;
-                    gate = tile[0]; up = tile[64];
+                    const float2 *row = reinterpret_cast<const float2 *>(smem + (size_t)c * 512) + lane;
+                    g0 = row[0].x; g1 = row[0].y; u0 = row[32].x; u1 = row[32].y;
                 } else {
                     for (int q = 0; q < cs; ++q) {
-                        const uint32_t peer = map_to_cta(at, q);
-                        gate += ld_cluster(peer); up += ld_cluster(peer + 256);
+                        const uint32_t peer = map_to_cta(base + c * 512, q);
+                        const float2 a = ld_cluster2(peer), b = ld_cluster2(peer + 256);
+                        g0 += a.x; g1 += a.y; u0 += b.x; u1 += b.y;
                     }
                 }
-                const bool member = p.mask == nullptr || (p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1);
-                const float a = member ? silu_f(gate) * up : 0.f;
-                const uint32_t byte = mx_scale_byte<true>(__reduce_max_sync(0xffffffffu, abs_bits(a)));
-                const uint8_t v = to_e4m3(byte == 255 ? 0.f : a * mx_inverse(byte));
-                p.a[(size_t)t * p.cap * 128 + entry * 128 + half * 64 + b * 32 + lane] = v;
+                const bool member = p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1);
+                float a0 = member ? silu_f(g0) * u0 : 0.f, a1 = member ? silu_f(g1) * u1 : 0.f;
+                uint32_t m = max(abs_bits(a0), abs_bits(a1));
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const uint32_t byte = mx_scale_byte<true>(m);
+                const float inv = mx_inverse(byte);
+                a0 = byte == 255 ? 0.f : a0 * inv; a1 = byte == 255 ? 0.f : a1 * inv;
+                reinterpret_cast<uint16_t *>(p.a + (size_t)t * p.cap * 128 + entry * 128 + half * 64)[lane] = pack_e4m3x2(a0, a1);
+                const uint32_t other = __shfl_down_sync(0xffffffffu, byte, 16);
                 if (lane == 0)
-                    p.a_scales[((size_t)(t >> 7) * p.cap + entry) * kMxTileBytes + (t & 31) * 16 + ((t & 127) >> 5) * 4 + half * 2 + b] = (uint8_t)byte;
+                    *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(t >> 7) * p.cap + entry) * kMxTileBytes + (t & 31) * 16 + ((t & 127) >> 5) * 4 + half * 2) =
+                        (uint16_t)(byte | other << 8);
             }
         }
         if (cs > 1) cluster_sync_all();      // peers are done with this CTA's tile
@@ -297,31 +351,55 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
     mx_teardown(&bars, cols);
 }
 
-// Grid (cluster, d / 128, token tiles): the CTAs of a cluster split the list.
+// Grid (cluster, d / 128, token tiles): the CTAs of a cluster split the list.  Weights depend on the list alone: where gate/up, which is still
+// running, has said that it stands, their loads start before the wait for gate/up's result.
 __global__ void __launch_bounds__(kMxThreads)
 mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const MxArgs p) {
     __shared__ MxBars bars;
-    const int cs = gridDim.x, rank = blockIdx.x, z = blockIdx.z, cols = mx_tmem_cols(p.tile, p.stages);
-    uint8_t *smem = mx_setup(&bars, p.stages, cols);
-    pdl_wait();
-    pdl_launch_dependents();
-    const int n = ld_dep(p.count);
-    const int columns = min(p.tile, (p.B - z * p.tile + 15) & ~15);
+    const int cs = gridDim.x, rank = blockIdx.x, z = blockIdx.z, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *smem = mx_setup(&bars, p.stages, cols, &wmap, &xmap);
+    if (threadIdx.x == 0) {
+        unsigned ready;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(ready) : "l"(p.ready) : "memory");
+        bars.all[0] = ready;
+    }
+    __syncthreads();
+    if (bars.all[0] == 0) pdl_wait();
+    if (threadIdx.x == 0) bars.count = ld_dep(p.count);
+    if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
+    __syncthreads();
+    const int n = bars.count;
+    const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
     const MxRange r = {n * rank / cs, n * (rank + 1) / cs - n * rank / cs};
-    mx_mainloop<true>(&wmap, &xmap, p, smem, &bars, (int64_t)blockIdx.y * p.G, r, z, columns);
+    if (warp == 0) {
+        if (lane == 0) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y * p.G, r);
+        __syncwarp();
+        pdl_wait();
+    } else {
+        pdl_wait();
+        pdl_launch_dependents();
+        if (warp == 3 && lane == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) *p.ready = 0;
+        if (warp == 1) {
+            if (lane == 0) mx_products(p, smem, &bars, r, columns);
+        } else if (warp == 2) {
+            if (lane == 0) mx_load_tokens(&xmap, p, smem, &bars, r, z, p.cap);
+        } else if (warp >= 4) {
+            mx_spill(p, smem, &bars, r, valid);
+        }
+        __syncwarp();
+    }
     if (cs > 1) cluster_sync_all();
-    const int e = (int)(threadIdx.x >> 5) - 2, lane = threadIdx.x & 31;
-    if (e >= 0) {
+    if (warp >= 4) {
         if (cs == 1) epilogue_sync();
-        const uint32_t base = smem_u32(smem);
-        for (int c = e * cs + rank; c < columns && z * p.tile + c < p.B; c += kMxEpiWarps * cs) {
-            const uint32_t at = base + (uint32_t)(c * 128 + lane * 4) * 4;
+        const uint32_t base = smem_u32(smem) + lane * 16;
+#pragma unroll 2
+        for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (cs == 1) {
-                v = *reinterpret_cast<const float4 *>(smem + (size_t)(c * 128 + lane * 4) * 4);
+                v = *reinterpret_cast<const float4 *>(smem + (size_t)c * 512 + lane * 16);
             } else {
                 for (int q = 0; q < cs; ++q) {
-                    const float4 u = ld_cluster4(map_to_cta(at, q));
+                    const float4 u = ld_cluster4(map_to_cta(base + c * 512, q));
                     v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
                 }
             }
@@ -332,25 +410,6 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     }
     if (cs > 1) cluster_sync_all();
     mx_teardown(&bars, cols);
-}
-
-// Matrix of bytes [rows, inner]: boxes of 128 bytes x box_rows, 128-byte swizzle.
-bool make_map_bytes(CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows, uint32_t box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (fn == nullptr) return false;
-    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {inner};
-    const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// Packed weight tiles, seen as rows of 128 four-bit elements: a box is a tile.
-bool make_map_tiles(CUtensorMap *map, const void *base, uint64_t tiles) {
-    EncodeTiledFn fn = encode_fn();
-    if (fn == nullptr) return false;
-    const cuuint64_t dims[2] = {128, tiles * 128}, strides[1] = {64};
-    const cuuint32_t box[2] = {128, 128}, estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 cudaError_t launch_clusters(void (*kernel)(const CUtensorMap, const CUtensorMap, const MxArgs), dim3 grid, size_t smem, cudaStream_t st,
@@ -374,7 +433,7 @@ cs_status prepare_mx_ffn(cs_plan *plan) {
     for (auto *k : {mx_gateup_kernel, mx_down_kernel})
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxSmemOne) != cudaSuccess || prefer_shared(k) != cudaSuccess)
             return CS_ERR_CUDA;
-    return prefer_shared(mx_list_kernel) == cudaSuccess ? CS_OK : CS_ERR_CUDA;
+    return prefer_shared(mx_list_kernel) == cudaSuccess ? prepare_mx_wide(plan) : CS_ERR_CUDA;
 }
 
 cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const uint8_t *s, const int32_t *support, bool shared,
@@ -382,6 +441,7 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int d = plan->cfg.d, k = plan->cfg.k, G = plan->G, kb = d / 128;
     const int cap = shared ? k : (int)min((int64_t)G, (int64_t)B * k);
     const int rows = shared ? 1 : B;
+    const bool wide = B > kMxNarrowTokens;
     const int tile = min(kMxMaxTile, (B + 15) / 16 * 16), tiles = (B + tile - 1) / tile;
     const bool two = tile <= 128;                        // two CTAs on an SM
     const int room = (two ? kMxSmemTwo : kMxSmemOne) - 1024 - (int)sizeof(MxBars) - 64;
@@ -389,18 +449,24 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const size_t smem = 1024 + (size_t)max(stages * mx_stage_bytes(tile), tile * 512);
     const int slots = plan->sm_count * (two ? 2 : 1);
     CUtensorMap wg, wd, xm, am;
-    if (!make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb) || !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G) ||
-        !make_map_bytes(&xm, q, d, B, tile) || !make_map_bytes(&am, plan->mx_a, (uint64_t)cap * 128, B, tile)) {
+    if (!wide && (!make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb) || !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G) ||
+        !make_map_bytes(&xm, q, d, B, tile) || !make_map_bytes(&am, plan->mx_a, (uint64_t)cap * 128, B, tile))) {
         snprintf(plan->cuda_error, sizeof plan->cuda_error, "cuTensorMapEncodeTiled failed");
         return CS_ERR_CUDA;
     }
-    cudaError_t e = launch_pdl(true, mx_list_kernel, dim3(1), dim3((int)min((int64_t)1024, max((int64_t)128, ((int64_t)rows * k + 31) / 32 * 32))), 0, st, support, rows, k, G,
-                               shared ? nullptr : plan->mask, plan->glist, plan->nu, plan->status);
-    if (e != cudaSuccess) return record_cuda(plan, e, "mx_list_kernel");
     MxArgs p;
-    p.w_scales = L->gate_up_scales; p.x_scales = s; p.list = plan->glist; p.count = plan->nu; p.mask = shared ? nullptr : plan->mask;
+    p.support = support; p.list = plan->glist; p.count = plan->nu; p.ready = plan->mask_count; p.mask = plan->mask;
+    p.w_scales = L->gate_up_scales; p.x_scales = s;
     p.a = plan->mx_a; p.a_scales = plan->mx_a_scales; p.out = static_cast<__nv_bfloat16 *>(out); p.status = plan->status;
-    p.B = B; p.d = d; p.G = G; p.cap = cap; p.tile = tile; p.stages = stages; p.w_once = tiles == 1;
+    p.B = B; p.d = d; p.G = G; p.k = k; p.cap = cap; p.tile = tile; p.stages = stages; p.shared = shared; p.w_once = tiles == 1;
+    p.fold = !wide && (int64_t)rows * k <= kMxFoldEntries;
+    cudaError_t e;
+    if (!p.fold) {
+        e = launch_pdl(true, mx_list_kernel, dim3(1), dim3(1024), 0, st, support, rows, k, G, plan->mask, plan->glist, plan->nu, plan->status);
+        if (e != cudaSuccess) return record_cuda(plan, e, "mx_list_kernel");
+        plan->launches += 1;
+    }
+    if (wide) return launch_mx_wide(plan, L, q, p, st);
     int cs = 1;
     while (cs < kMxMaxCluster && 2 * cap * tiles * cs * 2 <= slots && kb / (cs * 2) >= 4) cs *= 2;
     e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap, tiles), smem, st, wg, xm, p);
@@ -409,7 +475,7 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     cs = max(1, min(min(kMxMaxCluster, cap), slots / (kb * tiles)));
     e = launch_clusters(mx_down_kernel, dim3(cs, kb, tiles), smem, st, wd, am, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_down_kernel");
-    plan->launches += 3;
+    plan->launches += 2;
     return CS_OK;
 }
 

@@ -1,0 +1,384 @@
+// The FFN on microscaled operands for batches beyond one tile of mx_ffn.cu and for prompts, on pairs of CTAs.
+//
+//   mx_wide_kernel<false>   gate/up: an item is 256 tokens x one group (128 channels of W_gate and of W_up)
+//   mx_wide_kernel<true>    down: an item is 256 tokens x 256 (or 192) columns of the output, or a part of the list of it
+//   mx_wide_sum_kernel      adds the parts
+//
+// Here the tensor pipe is the bound, and before it what an SM can draw from L2: a single CTA of 128 weight rows x 256 tokens takes 41 KB for 512
+// cycles of products.  A cluster of two CTAs issues one instruction of 256 x 256 (cta_group::2): each brings 128 tokens and 128 weight
+// rows, 25 KB for the same 512 cycles.  Tokens are the M side, so a tensor-memory lane is a token and a row of 32 neighbouring columns in it a
+// block of channels: the epilogue finds a block's largest element, silu's two factors and the bytes it writes in one thread's registers.  A packed
+// gate/up tile (64 rows of W_gate, the same 64 of W_up) is one CTA's half of the columns.
+//
+// The kernel is persistent, one pair of CTAs on two SMs, and the ring of loads runs on across items.  One accumulator of 256 columns (the scales need some of
+// the other 256): the epilogue takes it into registers, 128 a thread, hands it back, and does its arithmetic while the next item's products run.
+#include <stdio.h>
+
+#include "mx_core.cuh"
+
+namespace cs {
+
+namespace {
+
+constexpr int kWideStages = 6;
+constexpr int kWideStageBytes = 128 * 128 + kMxWBytes + 3 * kMxTileBytes + 512;     // tokens, weights, scales: a multiple of 1024
+constexpr int kWideEpiWarps = 8;
+constexpr int kWideThreads = 128 + 32 * kWideEpiWarps;    // token loads, products, weight loads, one idle warp; epilogue
+constexpr int kWideTokens = 256;
+static_assert(kWideStageBytes % 1024 == 0, "operands stand on 1024-byte boundaries");
+
+struct WideArgs {
+    MxArgs p;
+    int ztiles;        // token tiles
+    int width;         // output columns of a down item, 256 or 192
+    int splits;        // parts of the list a down item is cut into; > 1: f32 results to `partial`
+    float *partial;    // [item, split][256 tokens][256 columns]
+};
+
+struct WideBars {
+    uint64_t full[kWideStages], empty[kWideStages], acc_full, acc_empty;
+    uint32_t tmem, aborted;
+    int32_t list[kMaxG], count;
+};
+
+// Instruction descriptor: e4m3 (tokens) x e2m1 (weights) with block scales, M = 256 over the pair, n columns.
+__device__ __forceinline__ uint32_t wide_idesc(int n, int kk) {
+    return ((uint32_t)kk << 4) | (5u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | (2u << 27) | ((uint32_t)kk << 29);
+}
+__device__ __forceinline__ void wide_copy_scales(uint32_t taddr, uint32_t saddr) {     // the same offsets in both CTAs
+    const uint64_t desc = (uint64_t)((saddr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void wide_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+// What pair `i` of an item index works on.
+struct WideItem {
+    int z, col;            // token tile; list entry (gate/up) or first output column (down)
+    int first, n, part;    // its k blocks
+};
+template <bool DOWN> __device__ __forceinline__ int wide_items(const WideArgs &w, int count) {
+    return w.ztiles * (DOWN ? (w.p.d + w.width - 1) / w.width * w.splits : count);
+}
+template <bool DOWN> __device__ __forceinline__ WideItem wide_item(const WideArgs &w, int count, int i) {
+    WideItem t;
+    const int across = DOWN ? (w.p.d + w.width - 1) / w.width : count;
+    t.part = DOWN ? i % w.splits : 0;
+    const int q = DOWN ? i / w.splits : i;
+    t.z = q / across;
+    t.col = (q - t.z * across) * (DOWN ? w.width : 1);
+    const int k = DOWN ? count : w.p.d >> 7, s = DOWN ? w.splits : 1;
+    t.first = k * t.part / s;
+    t.n = k * (t.part + 1) / s - t.first;
+    return t;
+}
+
+template <bool DOWN> __global__ void __launch_bounds__(kWideThreads, 1)
+mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xs, const __grid_constant__ CUtensorMap tm_w,
+               const __grid_constant__ CUtensorMap tm_ws, const WideArgs w) {
+    extern __shared__ uint8_t raw[];
+    __shared__ WideBars bars;
+    const MxArgs &p = w.p;
+    const uint32_t rank = cluster_ctarank();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kWideStages; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
+        mbar_init(&bars.acc_full, 1);
+        mbar_init(&bars.acc_empty, 2 * kWideEpiWarps);
+        bars.aborted = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (const CUtensorMap *m : {&tm_x, &tm_xs, &tm_w, &tm_ws}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    }
+    if (warp == 1) {   // the same warp of both CTAs allocates for the pair
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();        // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    pdl_wait();
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) bars.count = ld_dep(p.count);
+    if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
+    __syncthreads();
+    const int count = bars.count, items = wide_items<DOWN>(w, count);
+    const int columns = DOWN ? w.width : 256, rows = columns >> 1;      // rows: the weight rows a CTA brings
+
+    if (warp == 0) {          // tokens, and the bytes both CTAs will bring
+        if (lane == 0) {
+            const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
+            const uint32_t bytes = 2 * (128 * 128 + rows * 64 + 3 * kMxTileBytes);
+            MxRing ring;
+            int fill = 0;
+            for (int i = pair; i < items; i += pairs) {
+                const WideItem t = wide_item<DOWN>(w, count, i);
+                const int chunk = 2 * t.z + (int)rank;
+                for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
+                    if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
+                    uint8_t *st = smem + ring.stage * kWideStageBytes;
+                    if (rank == 0) mbar_expect_tx(&bars.full[ring.stage], bytes);
+                    tma_load_2d_pair(st, &tm_x, j * 128, chunk * 128, full0 + 8u * ring.stage);
+                    tma_load_2d_pair(st + 128 * 128 + kMxWBytes, &tm_xs, 0, chunk * (DOWN ? p.cap : p.d >> 7) + j, full0 + 8u * ring.stage);
+                    ring.next(kWideStages);
+                }
+            }
+        }
+    } else if (warp == 2) {   // weights
+        if (lane == 0) {
+            const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
+            MxRing ring;
+            int fill = 0;
+            for (int i = pair; i < items; i += pairs) {
+                const WideItem t = wide_item<DOWN>(w, count, i);
+                const int kb = p.d >> 7;
+                // tiles of 128 rows: gate/up's two halves of a group; the output's 128-column tiles, of which the last may be missing
+                const int row0 = DOWN ? t.col + (int)rank * rows : 0;
+                const int tile0 = DOWN ? t.col >> 7 : 2 * bars.list[t.col];
+                const int tile1 = DOWN ? min(tile0 + 1, kb - 1) : tile0 + 1;
+                for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
+                    if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
+                    uint8_t *st = smem + ring.stage * kWideStageBytes + 128 * 128;
+                    const uint32_t full = full0 + 8u * ring.stage;
+                    const int pitch = DOWN ? p.G : kb, at = DOWN ? bars.list[j] : j;
+                    if (!DOWN || w.width == 256) {
+                        tma_load_2d_pair(st, &tm_w, 0, ((rank ? tile1 : tile0) * pitch + at) * 128, full);
+                    } else {
+                        for (int b = 0; b < 3; ++b) {      // 96 rows from wherever they stand, 32 at a time
+                            const int row = row0 + 32 * b;
+                            tma_load_2d_pair(st + 32 * 128 * b, &tm_w, 0, (min(row >> 7, kb - 1) * pitch + at) * 128 + (row & 127), full);
+                        }
+                    }
+                    tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, &tm_ws, 0, tile0 * pitch + at, full);
+                    tma_load_2d_pair(st + kMxWBytes + 2 * kMxTileBytes, &tm_ws, 0, tile1 * pitch + at, full);
+                    ring.next(kWideStages);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            uint32_t idesc[4];
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) idesc[kk] = wide_idesc(columns, kk);
+            const uint32_t base = smem_u32(smem), tmem = bars.tmem;
+            MxRing ring;
+            int turn = 0;
+            for (int i = pair; i < items; i += pairs) {
+                const WideItem t = wide_item<DOWN>(w, count, i);
+                if (t.n == 0) continue;
+                const uint32_t shift = DOWN ? (uint32_t)(t.col & 127) >> 5 : 0;     // the first column's place in its tile of scales
+                if (turn > 0 && !mx_wait(&bars.acc_empty, (turn - 1) & 1, &bars.aborted, p.status)) goto done;
+                tc_fence_after();
+                for (int j = 0; j < t.n; ++j) {
+                    if (!mx_wait(&bars.full[ring.stage], ring.phase, &bars.aborted, p.status)) goto done;
+                    tc_fence_after();
+                    const uint32_t a = base + ring.stage * kWideStageBytes, b = a + 128 * 128, sc = b + kMxWBytes;
+                    const uint32_t sa = tmem + 256 + ring.stage * 12, sb = sa + 4;
+                    wide_copy_scales(sa, sc);
+                    wide_copy_scales(sb, sc + kMxTileBytes);
+                    wide_copy_scales(sb + 4, sc + 2 * kMxTileBytes);
+                    const uint64_t ad = desc_sw128(a, 0), bd = desc_sw128(b, 0);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) wide_mma(tmem, ad + 2 * kk, bd + 2 * kk, idesc[kk], sa, sb + shift, (j | kk) != 0);
+                    tc_commit_pair(&bars.empty[ring.stage]);
+                    ring.next(kWideStages);
+                }
+                tc_commit_pair(&bars.acc_full);
+                ++turn;
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp >> 2) - 1;      // lanes and half of the columns
+        const uint32_t empty0 = map_to_cta(smem_u32(&bars.acc_empty), 0);
+        int turn = 0;
+        for (int i = pair; i < items; i += pairs) {
+            __syncwarp();      // lanes without a token skip the end of an item
+            const WideItem t = wide_item<DOWN>(w, count, i);
+            const int token = t.z * kWideTokens + (int)rank * 128 + quarter * 32 + lane;
+            const int blocks = rows >> 5;                          // of 32 columns
+            uint32_t v[4][32];
+            if (t.n > 0) {
+                if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
+                tc_fence_after();
+                const uint32_t at = bars.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * rows);
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (b < blocks) tc_ld32(at + 32 * b, v[b]);
+                tc_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(empty0);
+                ++turn;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[b][c] = 0;
+            }
+            if (token >= p.B) continue;
+            if constexpr (!DOWN) {
+                const int g = bars.list[t.col];
+                const bool member = p.shared || (ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1);
+                uint32_t scales = 0;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {      // in place: the registers are what there is
+                        const float a = member ? silu_f(__uint_as_float(v[b][c])) * __uint_as_float(v[b + 2][c]) : 0.f;
+                        v[b][c] = __float_as_uint(a);
+                        m = max(m, abs_bits(a));
+                    }
+                    const uint32_t byte = mx_scale_byte<true>(m);
+                    const float inv = mx_inverse(byte);
+                    uint32_t o[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        o[c] = byte == 255 ? 0u : pack_e4m3(__uint_as_float(v[b][4 * c]) * inv, __uint_as_float(v[b][4 * c + 1]) * inv,
+                                                            __uint_as_float(v[b][4 * c + 2]) * inv, __uint_as_float(v[b][4 * c + 3]) * inv);
+                    store32(p.a + (size_t)token * p.cap * 128 + t.col * 128 + half * 64 + b * 32, o);
+                    scales |= byte << (8 * b);
+                }
+                *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(token >> 7) * p.cap + t.col) * kMxTileBytes + (token & 31) * 16 +
+                                              ((token & 127) >> 5) * 4 + half * 2) = (uint16_t)scales;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int col = t.col + half * rows + 32 * b;
+                    if (b >= blocks || col >= p.d) break;
+                    if (w.splits == 1) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {      // the caller's rows are 16-byte aligned
+                            __nv_bfloat162 f[4];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                f[c] = __floats2bfloat162_rn(__uint_as_float(v[b][8 * h + 2 * c]), __uint_as_float(v[b][8 * h + 2 * c + 1]));
+                            *reinterpret_cast<uint4 *>(p.out + (size_t)token * p.d + col + 8 * h) = *reinterpret_cast<const uint4 *>(f);
+                        }
+                    } else {
+                        float *to = w.partial + ((size_t)i * kWideTokens + token - t.z * kWideTokens) * 256 + half * rows + 32 * b;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            uint32_t o[8];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) o[c] = v[b][8 * h + c];
+                            store32(to + 8 * h, o);
+                        }
+                    }
+                }
+            }
+        }
+    }
+done:
+    __syncwarp();
+    // Neither CTA leaves (or frees tensor memory) while the other may still read its shared memory or signal its barriers; every wait above
+    // is bounded, so both reach this point.
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(bars.tmem), "r"(512) : "memory");
+    }
+}
+
+// out[t, c] = the sum of an item's parts, in their order.  Four columns a thread.
+__global__ void __launch_bounds__(256)
+mx_wide_sum_kernel(const WideArgs w) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int across = (w.p.d + w.width - 1) / w.width, d4 = w.p.d >> 2;
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= w.p.B * d4) return;
+    const int t = i / d4, c = (i - t * d4) * 4, z = t / kWideTokens, x = c / w.width;
+    const float *from = w.partial + ((size_t)(z * across + x) * w.splits * kWideTokens + t - z * kWideTokens) * 256 + c - x * w.width;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < w.splits; ++s) {
+        const float4 u = ld_dep4(from + (size_t)s * kWideTokens * 256);
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(w.p.out + (size_t)t * w.p.d + c) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+}
+
+// Tiles of 512 scales, one box each.
+bool make_map_scales(CUtensorMap *map, const void *base, uint64_t tiles) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {128, tiles}, strides[1] = {kMxTileBytes};
+    const cuuint32_t box[2] = {128, 1}, estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr size_t kWideSmem = 1024 + (size_t)kWideStages * kWideStageBytes;
+
+template <bool DOWN>
+cudaError_t launch_wide(int pairs, cudaStream_t st, const CUtensorMap &x, const CUtensorMap &xs, const CUtensorMap &wt, const CUtensorMap &ws, const WideArgs &w) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = kWideSmem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, mx_wide_kernel<DOWN>, x, xs, wt, ws, w);
+}
+
+}  // namespace
+
+cs_status prepare_mx_wide(cs_plan *plan) {
+    (void)plan;
+    for (auto *k : {mx_wide_kernel<false>, mx_wide_kernel<true>})
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kWideSmem) != cudaSuccess || prefer_shared(k) != cudaSuccess)
+            return CS_ERR_CUDA;
+    return prefer_shared(mx_wide_sum_kernel) == cudaSuccess ? CS_OK : CS_ERR_CUDA;
+}
+
+size_t mx_wide_partial_bytes(const cs_plan *plan) { return (size_t)(plan->sm_count / 2) * kWideTokens * 256 * sizeof(float); }
+
+cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const MxArgs &args, cudaStream_t st) {
+    const int kb = args.d / 128, G = args.G, B = args.B, chunks = (B + 127) / 128, pairs = plan->sm_count / 2;
+    WideArgs w;
+    w.p = args;
+    w.ztiles = (B + kWideTokens - 1) / kWideTokens;
+    w.partial = plan->mx_partial;
+    w.splits = 1;
+    // Output columns of a down item: the width whose rounds over the pairs cost least (13B shape, 2048 tokens: 160 items of 256 are three rounds, 216
+    // of 192 three rounds of 3/4).
+    auto cost = [&](int width) { return (((args.d + width - 1) / width * w.ztiles + pairs - 1) / pairs) * width; };
+    w.width = cost(192) < cost(256) ? 192 : 256;
+    const int items = (args.d + w.width - 1) / w.width * w.ztiles;
+    // Fewer items than pairs: cut the list, into parts of at least four k blocks
+    if (2 * items <= pairs) w.splits = max(1, min(min(pairs / items, 8), args.cap / 4));
+    CUtensorMap x, xs, wg, wgs, a, as, wd, wds;
+    if (!make_map_bytes(&x, q, args.d, B, 128) || !make_map_scales(&xs, args.x_scales, (uint64_t)chunks * kb) ||
+        !make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb, 128) || !make_map_scales(&wgs, L->gate_up_scales, (uint64_t)2 * G * kb) ||
+        !make_map_bytes(&a, plan->mx_a, (uint64_t)args.cap * 128, B, 128) || !make_map_scales(&as, plan->mx_a_scales, (uint64_t)chunks * args.cap) ||
+        !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G, w.width == 256 ? 128 : 32) || !make_map_scales(&wds, L->down_scales, (uint64_t)kb * G)) {
+        snprintf(plan->cuda_error, sizeof plan->cuda_error, "cuTensorMapEncodeTiled failed");
+        return CS_ERR_CUDA;
+    }
+    cudaError_t e = launch_wide<false>(pairs, st, x, xs, wg, wgs, w);
+    if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<gate/up>");
+    e = launch_wide<true>(min(pairs, items * w.splits), st, a, as, wd, wds, w);
+    if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<down>");
+    plan->launches += 2;
+    if (w.splits > 1) {
+        e = launch_pdl(true, mx_wide_sum_kernel, dim3((B * (args.d / 4) + 255) / 256), dim3(256), 0, st, w);
+        if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_sum_kernel");
+        plan->launches += 1;
+    }
+    return CS_OK;
+}
+
+}  // namespace cs
