@@ -31,6 +31,14 @@ namespace {
 
 constexpr int kMxWBytes = 128 * 128;                 // a weight tile in shared memory
 constexpr int kMxWLoad = 128 * 64;                   // ... and in memory, which is what the barrier counts
+// One thread of a converged warp.  The compiler knows that an elect.sync branch is taken by a single thread; behind `lane == 0` it
+// wraps every instruction that takes its operands from uniform registers (tcgen05.mma, TMA) in a loop over the active threads: 95 cycles to issue
+// an MMA against 46.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
 // Ring position without divisions: the issue of a k block's copies is what a CTA's weight stream waits for first.
 struct MxRing {
     int stage = 0;

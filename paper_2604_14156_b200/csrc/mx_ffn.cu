@@ -300,11 +300,11 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
         const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
         const MxRange r = {kb * rank / cs, kb * (rank + 1) / cs - kb * rank / cs};
         if (warp == 0) {
-            if (lane == 0) mx_load_weights<false>(&wmap, p, smem, &bars, (2 * g + half) * kb, r);
+            if (elect_one()) mx_load_weights<false>(&wmap, p, smem, &bars, (2 * g + half) * kb, r);
         } else if (warp == 1) {
-            if (lane == 0) mx_products(p, smem, &bars, r, columns);
+            if (elect_one()) mx_products(p, smem, &bars, r, columns);
         } else if (warp == 2) {
-            if (lane == 0) mx_load_tokens(&xmap, p, smem, &bars, r, z, kb);
+            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, z, kb);
         } else if (warp >= 4) {
             if (p.fold && !p.shared)      // while the products run: who uses this group
                 for (int t = threadIdx.x - 128; t < valid * p.k; t += 32 * kMxEpiWarps)
@@ -372,7 +372,7 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
     const MxRange r = {n * rank / cs, n * (rank + 1) / cs - n * rank / cs};
     if (warp == 0) {
-        if (lane == 0) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y * p.G, r);
+        if (elect_one()) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y * p.G, r);
         __syncwarp();
         pdl_wait();
     } else {
@@ -380,9 +380,9 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         pdl_launch_dependents();
         if (warp == 3 && lane == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) *p.ready = 0;
         if (warp == 1) {
-            if (lane == 0) mx_products(p, smem, &bars, r, columns);
+            if (elect_one()) mx_products(p, smem, &bars, r, columns);
         } else if (warp == 2) {
-            if (lane == 0) mx_load_tokens(&xmap, p, smem, &bars, r, z, p.cap);
+            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, z, p.cap);
         } else if (warp >= 4) {
             mx_spill(p, smem, &bars, r, valid);
         }

@@ -114,7 +114,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     const int columns = DOWN ? w.width : 256, rows = columns >> 1;      // rows: the weight rows a CTA brings
 
     if (warp == 0) {          // tokens, and the bytes both CTAs will bring
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
             const uint32_t bytes = 2 * (128 * 128 + rows * 64 + 3 * kMxTileBytes);
             MxRing ring;
@@ -133,7 +133,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             }
         }
     } else if (warp == 2) {   // weights
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
             MxRing ring;
             int fill = 0;
@@ -164,7 +164,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             uint32_t idesc[4];
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) idesc[kk] = wide_idesc(columns, kk);
