@@ -58,6 +58,15 @@ __device__ __forceinline__ uint16_t pack_e4m3x2(float a, float b) {
     return r;
 }
 
+// silu(gate) up.  The fast exponential and division: 2^-20 of the result, against the 2^-4 of the rounding that follows.
+__device__ __forceinline__ float swiglu(float gate, float up) { return __fdividef(gate, 1.f + __expf(-gate)) * up; }
+// max(m, |v|), NaN where either is.
+__device__ __forceinline__ float max_abs(float m, float v) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(v)));
+    return r;
+}
+
 // mx_norm.cu
 cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *delta, int delta_dtype, const float *gamma, int B,
                          void *x_out, float *n_out, uint8_t *q, uint8_t *s, cudaStream_t st);

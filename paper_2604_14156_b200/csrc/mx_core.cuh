@@ -19,6 +19,7 @@ struct MxArgs {
     int B, d, G, k;
     int cap;                        // groups the list can hold: pitch of a and its scales
     int tile, stages;               // tokens of a tile, ring stages
+    int entries;                    // of the support
     int shared, fold;               // one support for all tokens; gate/up makes the list
     int w_once;                     // weights are read by one token tile only
 };
@@ -29,6 +30,7 @@ cs_status prepare_mx_wide(cs_plan *plan);
 
 namespace {
 
+constexpr int kMxFoldEntries = 2048, kWideFoldEntries = 8192;   // up to this many support entries gate/up makes the list itself
 constexpr int kMxWBytes = 128 * 128;                 // a weight tile in shared memory
 constexpr int kMxWLoad = 128 * 64;                   // ... and in memory, which is what the barrier counts
 // One thread of a converged warp.  The compiler knows that an elect.sync branch is taken by a single thread; behind `lane == 0` it
@@ -38,6 +40,46 @@ __device__ __forceinline__ bool elect_one() {
     uint32_t one;
     asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
     return one != 0;
+}
+// Marks the groups of `n` support entries in `all` (cleared before), with all `threads` threads of a CTA.
+__device__ __forceinline__ void mx_mark(const int32_t *support, int n, int G, uint32_t *all, int threads) {
+    for (int i0 = threadIdx.x; i0 < n; i0 += 8 * threads) {
+        int g[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) g[u] = i0 + u * threads < n ? ld_dep(support + i0 + u * threads) : -1;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u * threads;
+            if (i >= n) break;
+            if (g[u] >= 0 && g[u] < G) {
+                const uint32_t bit = 1u << (g[u] & 31);
+                if (!(*reinterpret_cast<volatile uint32_t *>(&all[g[u] >> 5]) & bit)) atomicOr(&all[g[u] >> 5], bit);
+            }
+        }
+    }
+}
+// Reports entries that are not ascending within rows of k, or outside [0, G): beside the products, by one warp of each of `parts` CTAs.
+__device__ __forceinline__ void mx_check(const int32_t *support, int n, int k, int G, int part, int parts, DeviceStatus *status) {
+    bool bad = false;
+    for (int i = part * 32 + (threadIdx.x & 31); i < n; i += 32 * parts) {
+        const int g = ld_dep(support + i);
+        bad |= g >= G || g <= (i % k != 0 ? ld_dep(support + i - 1) : -1);
+    }
+    if (bad) atomicCAS(&status->code, 0, (int)CS_ERR_SUPPORT);
+}
+// The marked groups in ascending order, and their number (threads 0..127 of the CTA).
+__device__ __forceinline__ void mx_list_of(const uint32_t (&all)[4], int32_t *list, int32_t *count) {
+    if (threadIdx.x < 128) {
+        const int g = threadIdx.x, w = g >> 5;
+        int before = 0, n = 0;
+        for (int i = 0; i < 4; ++i) {
+            if (i < w) before += __popc(all[i]);
+            n += __popc(all[i]);
+        }
+        before += __popc(all[w] & ((1u << (g & 31)) - 1));
+        if (all[w] >> (g & 31) & 1) list[before] = g;
+        if (g == 0) *count = n;
+    }
 }
 // Ring position without divisions: the issue of a k block's copies is what a CTA's weight stream waits for first.
 struct MxRing {

@@ -27,7 +27,6 @@ constexpr int kMxMaxTile = 256;                      // tokens of a tile
 constexpr int kMxMaxStages = 8;
 constexpr int kMxMaxCluster = 8;
 constexpr int kMxNarrowTokens = 128;                 // larger batches take the pairs of mx_wide.cu
-constexpr int kMxFoldEntries = 2048;                 // up to this many support entries gate/up makes the list itself
 
 struct MxBars {
     uint64_t full[kMxMaxStages], empty[kMxMaxStages], acc;
@@ -78,20 +77,6 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     return v;
 }
 
-__device__ __forceinline__ void mx_list_of(const uint32_t (&all)[4], int32_t *list, int32_t *count) {
-    if (threadIdx.x < 128) {
-        const int g = threadIdx.x, w = g >> 5;
-        int before = 0, n = 0;
-        for (int i = 0; i < 4; ++i) {
-            if (i < w) before += __popc(all[i]);
-            n += __popc(all[i]);
-        }
-        before += __popc(all[w] & ((1u << (g & 31)) - 1));
-        if (all[w] >> (g & 31) & 1) list[before] = g;
-        if (g == 0) *count = n;
-    }
-}
-
 // One CTA: the union of all rows of `support`, the rows' membership bits (when mask != NULL), validation.  A thread per entry, so that all loads
 // of up to kMxListRows rows are in flight together.
 constexpr int kMxListRows = 512;
@@ -136,33 +121,6 @@ mx_list_kernel(const int32_t *support, int rows, int k, int G, uint32_t *mask, i
     mx_list_of(all, list, count);
 }
 
-// The union of `rows` rows of supports into bars->all, by all threads; `mine` (or -1): bars->bits says which rows hold that group.
-__device__ __forceinline__ void mx_union(const int32_t *support, int rows, int k, int G, MxBars *bars, int mine, DeviceStatus *status) {
-    for (int i = threadIdx.x; i < 4 + kMxMaxTile / 32; i += kMxThreads) (i < 4 ? bars->all[i] : bars->bits[i - 4]) = 0;
-    __syncthreads();
-    const int n = rows * k;
-    bool bad = false;
-    constexpr int kAhead = (kMxFoldEntries + kMxThreads - 1) / kMxThreads;
-    int g[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        const int i = threadIdx.x + u * kMxThreads;
-        g[u] = i < n ? ld_dep(support + i) : 0;
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        const int i = threadIdx.x + u * kMxThreads;
-        if (i < n) {
-            if (status != nullptr) bad |= g[u] >= G || g[u] <= (i % k != 0 ? ld_dep(support + i - 1) : -1);
-            if (g[u] >= 0 && g[u] < G) {
-                const uint32_t bit = 1u << (g[u] & 31);
-                if (!(*reinterpret_cast<volatile uint32_t *>(&bars->all[g[u] >> 5]) & bit)) atomicOr(&bars->all[g[u] >> 5], bit);
-            }
-        }
-    }
-    if (bad) atomicCAS(&status->code, 0, (int)CS_ERR_SUPPORT);
-    __syncthreads();
-}
 struct MxRange { int first, n; };
 
 // Three warps feed and run the products of k blocks [r.first, r.first + r.n) against token tile z.  Weight tile of k block j: wtile + j, or with DOWN
@@ -280,21 +238,26 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
     pdl_launch_dependents();
     const bool first = blockIdx.x + blockIdx.y + blockIdx.z == 0;
     if (p.fold) {
-        mx_union(p.support, p.shared ? 1 : p.B, p.k, p.G, &bars, -1, first ? p.status : nullptr);
+        if (threadIdx.x < 4 + kMxMaxTile / 32) (threadIdx.x < 4 ? bars.all[threadIdx.x] : bars.bits[threadIdx.x - 4]) = 0;
+        __syncthreads();
+        mx_mark(p.support, p.entries, p.G, bars.all, kMxThreads);
+        __syncthreads();
         mx_list_of(bars.all, bars.list, &bars.count);
-        __syncthreads();
-        if (first) {      // for the down product, which may read it once `ready` is set
-            if ((int)threadIdx.x < bars.count) p.list[threadIdx.x] = bars.list[threadIdx.x];
-            if (threadIdx.x == 0) *p.count = bars.count;
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
-        }
-    } else {
-        if (threadIdx.x == 0) { bars.count = ld_dep(p.count); bars.list[entry] = ld_dep(p.list + entry); }
-        __syncthreads();
-        if (first && threadIdx.x == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
+    } else if (threadIdx.x == 0) {
+        bars.count = ld_dep(p.count);
+        bars.list[entry] = ld_dep(p.list + entry);
     }
+    __syncthreads();
+    if (first && warp == 3) {      // beside the products: the list for the down product, which may read it once `ready` is set
+        if (p.fold) {
+            for (int i = lane; i < bars.count; i += 32) p.list[i] = bars.list[i];
+            if (lane == 0) *p.count = bars.count;
+            __threadfence();
+            __syncwarp();
+        }
+        if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
+    }
+    if (p.fold && warp == 3 && blockIdx.x + blockIdx.z == 0) mx_check(p.support, p.entries, p.k, p.G, blockIdx.y, gridDim.y, p.status);
     if (entry < bars.count) {      // the same in every CTA of a cluster
         const int g = bars.list[entry];
         const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
@@ -332,7 +295,7 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
                     }
                 }
                 const bool member = p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1);
-                float a0 = member ? silu_f(g0) * u0 : 0.f, a1 = member ? silu_f(g1) * u1 : 0.f;
+                float a0 = member ? swiglu(g0, u0) : 0.f, a1 = member ? swiglu(g1, u1) : 0.f;
                 uint32_t m = max(abs_bits(a0), abs_bits(a1));
 #pragma unroll
                 for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -459,7 +422,8 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     p.w_scales = L->gate_up_scales; p.x_scales = s;
     p.a = plan->mx_a; p.a_scales = plan->mx_a_scales; p.out = static_cast<__nv_bfloat16 *>(out); p.status = plan->status;
     p.B = B; p.d = d; p.G = G; p.k = k; p.cap = cap; p.tile = tile; p.stages = stages; p.shared = shared; p.w_once = tiles == 1;
-    p.fold = !wide && (int64_t)rows * k <= kMxFoldEntries;
+    p.entries = (int)min((int64_t)rows * k, (int64_t)1 << 30);
+    p.fold = p.entries <= (wide ? kWideFoldEntries : kMxFoldEntries);
     cudaError_t e;
     if (!p.fold) {
         e = launch_pdl(true, mx_list_kernel, dim3(1), dim3(1024), 0, st, support, rows, k, G, plan->mask, plan->glist, plan->nu, plan->status);

@@ -1,7 +1,7 @@
 // The FFN on microscaled operands for batches beyond one tile of mx_ffn.cu and for prompts, on pairs of CTAs.
 //
-//   mx_wide_kernel<false>   gate/up: an item is 256 tokens x one group (128 channels of W_gate and of W_up)
-//   mx_wide_kernel<true>    down: an item is 256 tokens x 256 (or 192) columns of the output, or a part of the list of it
+//   mx_wide_kernel<false, 4>  gate/up: an item is 256 tokens x one group (128 channels of W_gate and of W_up)
+//   mx_wide_kernel<true, .>  down: an item is 256 tokens x 256 (or 192) columns of the output, or a part of the list of it
 //   mx_wide_sum_kernel      adds the parts
 //
 // Here the tensor pipe is the bound, and before it what an SM can draw from L2: a single CTA of 128 weight rows x 256 tokens takes 41 KB for 512
@@ -32,12 +32,15 @@ struct WideArgs {
     int ztiles;        // token tiles
     int width;         // output columns of a down item, 256 or 192
     int splits;        // parts of the list a down item is cut into; > 1: f32 results to `partial`
+    int whole;         // the output's rows stand on 32-byte boundaries: whole sectors
+    const uint8_t *down_codes, *down_scales;
     float *partial;    // [item, split][256 tokens][256 columns]
 };
 
 struct WideBars {
     uint64_t full[kWideStages], empty[kWideStages], acc_full, acc_empty;
     uint32_t tmem, aborted;
+    uint32_t all[4];
     int32_t list[kMaxG], count;
 };
 
@@ -59,7 +62,11 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8]) {
                  ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
-// What pair `i` of an item index works on.
+__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
+// What item `i` is.
 struct WideItem {
     int z, col;            // token tile; list entry (gate/up) or first output column (down)
     int first, n, part;    // its k blocks
@@ -80,7 +87,8 @@ template <bool DOWN> __device__ __forceinline__ WideItem wide_item(const WideArg
     return t;
 }
 
-template <bool DOWN> __global__ void __launch_bounds__(kWideThreads, 1)
+// BLOCKS: 32-column blocks of a CTA's half of the columns.
+template <bool DOWN, int BLOCKS> __global__ void __launch_bounds__(kWideThreads, 1)
 mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xs, const __grid_constant__ CUtensorMap tm_w,
                const __grid_constant__ CUtensorMap tm_ws, const WideArgs w) {
     extern __shared__ uint8_t raw[];
@@ -107,11 +115,20 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     tc_fence_after();
     pdl_wait();
     pdl_launch_dependents();
-    if (threadIdx.x == 0) bars.count = ld_dep(p.count);
-    if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
+    if (p.fold) {
+        if (threadIdx.x < 4) bars.all[threadIdx.x] = 0;
+        __syncthreads();
+        mx_mark(p.support, p.entries, p.G, bars.all, kWideThreads);
+        __syncthreads();
+        mx_list_of(bars.all, bars.list, &bars.count);
+    } else {
+        if (threadIdx.x == 0) bars.count = ld_dep(p.count);
+        if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
+    }
     __syncthreads();
     const int count = bars.count, items = wide_items<DOWN>(w, count);
-    const int columns = DOWN ? w.width : 256, rows = columns >> 1;      // rows: the weight rows a CTA brings
+    constexpr int columns = 64 * BLOCKS, rows = columns >> 1;      // rows: the weight rows a CTA brings
+    if (!DOWN && p.fold && warp == 3) mx_check(p.support, p.entries, p.k, p.G, blockIdx.x, gridDim.x, p.status);
 
     if (warp == 0) {          // tokens, and the bytes both CTAs will bring
         if (elect_one()) {
@@ -136,7 +153,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
             MxRing ring;
-            int fill = 0;
+            int fill = 0, ahead = blockIdx.x;
             for (int i = pair; i < items; i += pairs) {
                 const WideItem t = wide_item<DOWN>(w, count, i);
                 const int kb = p.d >> 7;
@@ -149,7 +166,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                     uint8_t *st = smem + ring.stage * kWideStageBytes + 128 * 128;
                     const uint32_t full = full0 + 8u * ring.stage;
                     const int pitch = DOWN ? p.G : kb, at = DOWN ? bars.list[j] : j;
-                    if (!DOWN || w.width == 256) {
+                    if (BLOCKS == 4) {
                         tma_load_2d_pair(st, &tm_w, 0, ((rank ? tile1 : tile0) * pitch + at) * 128, full);
                     } else {
                         for (int b = 0; b < 3; ++b) {      // 96 rows from wherever they stand, 32 at a time
@@ -159,6 +176,12 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                     }
                     tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, &tm_ws, 0, tile0 * pitch + at, full);
                     tma_load_2d_pair(st + kMxWBytes + 2 * kMxTileBytes, &tm_ws, 0, tile1 * pitch + at, full);
+                    if (!DOWN && fill >= kWideStages && ahead < kb * count) {      // the down product's weights on their way to L2
+                        const size_t tile = (size_t)(ahead / count) * p.G + bars.list[ahead % count];
+                        prefetch_l2(w.down_codes + tile * kMxWLoad, kMxWLoad);
+                        prefetch_l2(w.down_scales + tile * kMxTileBytes, kMxTileBytes);
+                        ahead += gridDim.x;
+                    }
                     ring.next(kWideStages);
                 }
             }
@@ -203,15 +226,24 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             __syncwarp();      // lanes without a token skip the end of an item
             const WideItem t = wide_item<DOWN>(w, count, i);
             const int token = t.z * kWideTokens + (int)rank * 128 + quarter * 32 + lane;
-            const int blocks = rows >> 5;                          // of 32 columns
-            uint32_t v[4][32];
+            bool member = true;      // whether this token uses the group; found while the products run
+            if (!DOWN && !p.shared && token < p.B) {
+                const int g = bars.list[t.col];
+                if (p.fold) {
+                    member = false;
+                    for (int j = 0; j < p.k; ++j) member |= ld_dep(p.support + (size_t)token * p.k + j) == g;
+                } else {
+                    member = ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1;
+                }
+            }
+            __syncwarp();
+            uint32_t v[BLOCKS][32];
             if (t.n > 0) {
                 if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
                 tc_fence_after();
                 const uint32_t at = bars.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * rows);
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    if (b < blocks) tc_ld32(at + 32 * b, v[b]);
+                for (int b = 0; b < BLOCKS; ++b) tc_ld32(at + 32 * b, v[b]);
                 tc_wait_ld();
                 tc_fence_before();
                 __syncwarp();
@@ -219,30 +251,28 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                 ++turn;
             } else {
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int c = 0; c < 32; ++c) v[b][c] = 0;
             }
             if (token >= p.B) continue;
             if constexpr (!DOWN) {
-                const int g = bars.list[t.col];
-                const bool member = p.shared || (ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1);
                 uint32_t scales = 0;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    uint32_t m = 0;
+                    float m = 0.f;
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {      // in place: the registers are what there is
-                        const float a = member ? silu_f(__uint_as_float(v[b][c])) * __uint_as_float(v[b + 2][c]) : 0.f;
+                        const float a = swiglu(__uint_as_float(v[b][c]), __uint_as_float(v[b + 2][c]));
                         v[b][c] = __float_as_uint(a);
-                        m = max(m, abs_bits(a));
+                        m = max_abs(m, a);
                     }
-                    const uint32_t byte = mx_scale_byte<true>(m);
+                    const uint32_t byte = member ? mx_scale_byte<true>(__float_as_uint(m)) : 0u;
                     const float inv = mx_inverse(byte);
                     uint32_t o[8];
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
-                        o[c] = byte == 255 ? 0u : pack_e4m3(__uint_as_float(v[b][4 * c]) * inv, __uint_as_float(v[b][4 * c + 1]) * inv,
+                        o[c] = !member || byte == 255 ? 0u : pack_e4m3(__uint_as_float(v[b][4 * c]) * inv, __uint_as_float(v[b][4 * c + 1]) * inv,
                                                             __uint_as_float(v[b][4 * c + 2]) * inv, __uint_as_float(v[b][4 * c + 3]) * inv);
                     store32(p.a + (size_t)token * p.cap * 128 + t.col * 128 + half * 64 + b * 32, o);
                     scales |= byte << (8 * b);
@@ -251,12 +281,23 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                                               ((token & 127) >> 5) * 4 + half * 2) = (uint16_t)scales;
             } else {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                for (int b = 0; b < BLOCKS; ++b) {
                     const int col = t.col + half * rows + 32 * b;
-                    if (b >= blocks || col >= p.d) break;
-                    if (w.splits == 1) {
+                    if (col >= p.d) break;
+                    if (w.splits == 1 && w.whole) {
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) {      // the caller's rows are 16-byte aligned
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t o[8];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                const __nv_bfloat162 f = __floats2bfloat162_rn(__uint_as_float(v[b][16 * h + 2 * c]), __uint_as_float(v[b][16 * h + 2 * c + 1]));
+                                o[c] = *reinterpret_cast<const uint32_t *>(&f);
+                            }
+                            store32(p.out + (size_t)token * p.d + col + 16 * h, o);
+                        }
+                    } else if (w.splits == 1) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
                             __nv_bfloat162 f[4];
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
@@ -321,7 +362,7 @@ bool make_map_scales(CUtensorMap *map, const void *base, uint64_t tiles) {
 
 constexpr size_t kWideSmem = 1024 + (size_t)kWideStages * kWideStageBytes;
 
-template <bool DOWN>
+template <bool DOWN, int BLOCKS>
 cudaError_t launch_wide(int pairs, cudaStream_t st, const CUtensorMap &x, const CUtensorMap &xs, const CUtensorMap &wt, const CUtensorMap &ws, const WideArgs &w) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = kWideSmem; cfg.stream = st;
@@ -331,14 +372,14 @@ cudaError_t launch_wide(int pairs, cudaStream_t st, const CUtensorMap &x, const 
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, mx_wide_kernel<DOWN>, x, xs, wt, ws, w);
+    return cudaLaunchKernelEx(&cfg, mx_wide_kernel<DOWN, BLOCKS>, x, xs, wt, ws, w);
 }
 
 }  // namespace
 
 cs_status prepare_mx_wide(cs_plan *plan) {
     (void)plan;
-    for (auto *k : {mx_wide_kernel<false>, mx_wide_kernel<true>})
+    for (auto *k : {mx_wide_kernel<false, 4>, mx_wide_kernel<true, 4>, mx_wide_kernel<true, 3>})
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kWideSmem) != cudaSuccess || prefer_shared(k) != cudaSuccess)
             return CS_ERR_CUDA;
     return prefer_shared(mx_wide_sum_kernel) == cudaSuccess ? CS_OK : CS_ERR_CUDA;
@@ -352,7 +393,9 @@ cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, 
     w.p = args;
     w.ztiles = (B + kWideTokens - 1) / kWideTokens;
     w.partial = plan->mx_partial;
+    w.down_codes = L->down_codes; w.down_scales = L->down_scales;
     w.splits = 1;
+    w.whole = reinterpret_cast<uintptr_t>(args.out) % 32 == 0;
     // Output columns of a down item: the width whose rounds over the pairs cost least (13B shape, 2048 tokens: 160 items of 256 are three rounds, 216
     // of 192 three rounds of 3/4).
     auto cost = [&](int width) { return (((args.d + width - 1) / width * w.ztiles + pairs - 1) / pairs) * width; };
@@ -368,9 +411,9 @@ cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, 
         snprintf(plan->cuda_error, sizeof plan->cuda_error, "cuTensorMapEncodeTiled failed");
         return CS_ERR_CUDA;
     }
-    cudaError_t e = launch_wide<false>(pairs, st, x, xs, wg, wgs, w);
+    cudaError_t e = launch_wide<false, 4>(pairs, st, x, xs, wg, wgs, w);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<gate/up>");
-    e = launch_wide<true>(min(pairs, items * w.splits), st, a, as, wd, wds, w);
+    e = (w.width == 256 ? launch_wide<true, 4> : launch_wide<true, 3>)(min(pairs, items * w.splits), st, a, as, wd, wds, w);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<down>");
     plan->launches += 2;
     if (w.splits > 1) {
