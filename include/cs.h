@@ -362,8 +362,8 @@ cs_status cs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int32_t 
 
 /* Weights of one layer in the order cs_mx_ffn reads them (device pointers, caller-owned, written by cs_mx_pack): tiles of
  * 128 rows x 128 columns, the codes row by row (8192 bytes), the scales in tile order (512 bytes, see cs_mx_norm).
- * gate_up: for each 64 channels, for each 128 columns, a tile of 64 rows of W_gate and the same 64 of W_up.
- * down: for each 128 rows of W_down [d, d_ff], for each group, a tile.  Codes are 32-byte, scales 16-byte aligned. */
+ * gate_up: for each group, for each 128 columns, for each half of the group's channels, a tile of 64 rows of W_gate and the
+ * same 64 of W_up.  down: for each group, for each 128 rows of W_down [d, d_ff], a tile.  Codes are 32-byte, scales 16-byte aligned. */
 typedef struct {
     const uint8_t *gate_up_codes;   /* [d_ff * d]       bytes */
     const uint8_t *gate_up_scales;  /* [d_ff * d / 16]  */

@@ -123,8 +123,8 @@ mx_list_kernel(const int32_t *support, int rows, int k, int G, uint32_t *mask, i
 
 struct MxRange { int first, n; };
 
-// Three warps feed and run the products of k blocks [r.first, r.first + r.n) against token tile z.  Weight tile of k block j: wtile + j, or with DOWN
-// wtile + list[j].
+// Three warps feed and run the products of k blocks [r.first, r.first + r.n) against token tile z.  Weight tile of k block j: wtile + 2 j, or with DOWN
+// wtile + (d / 128) list[j].
 template <bool DOWN>
 __device__ __forceinline__ void mx_load_weights(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, int wtile, MxRange r) {
     const uint64_t policy = policy_evict_first();
@@ -134,7 +134,7 @@ __device__ __forceinline__ void mx_load_weights(const CUtensorMap *map, const Mx
         if (i >= p.stages && !mx_wait(&bars->empty[ring.stage], ring.phase ^ 1, &bars->aborted, p.status)) return;
         uint8_t *w = smem + ring.stage * stage_bytes;
         uint64_t *full = &bars->full[ring.stage];
-        const int tile = wtile + (DOWN ? bars->list[r.first + i] : r.first + i);
+        const int tile = DOWN ? wtile + bars->list[r.first + i] * (p.d >> 7) : wtile + 2 * (r.first + i);
         mbar_expect_tx(full, kMxWLoad + kMxTileBytes);
         if (p.w_once) tma_load_2d(w, map, 0, tile * 128, full, policy);
         else tma_load_2d(w, map, 0, tile * 128, full);
@@ -263,7 +263,7 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
         const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
         const MxRange r = {kb * rank / cs, kb * (rank + 1) / cs - kb * rank / cs};
         if (warp == 0) {
-            if (elect_one()) mx_load_weights<false>(&wmap, p, smem, &bars, (2 * g + half) * kb, r);
+            if (elect_one()) mx_load_weights<false>(&wmap, p, smem, &bars, 2 * g * kb + half, r);
         } else if (warp == 1) {
             if (elect_one()) mx_products(p, smem, &bars, r, columns);
         } else if (warp == 2) {
@@ -335,7 +335,7 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
     const MxRange r = {n * rank / cs, n * (rank + 1) / cs - n * rank / cs};
     if (warp == 0) {
-        if (elect_one()) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y * p.G, r);
+        if (elect_one()) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y, r);
         __syncwarp();
         pdl_wait();
     } else {

@@ -184,27 +184,28 @@ dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__
 }
 
 // Row-major codes and scales to the FFN's tiles of 128 rows x 128 columns (8 KB of codes, row by row, and 512 scales in tile order).
-// Gate and up share a tile: rows 0..63 are 64 channels of W_gate, rows 64..127 the same channels of W_up.
-__global__ void __launch_bounds__(256)
+// GATE_UP: tile (group, k block, half): rows 0..63 are 64 channels of W_gate, rows 64..127 the same channels of W_up; `inner` k blocks.
+// Otherwise tile (group, row tile): 128 rows of W_down, the group's 128 columns; `inner` row tiles.
+template <bool GATE_UP> __global__ void __launch_bounds__(256)
 pack_tiles_kernel(const uint8_t *__restrict__ c0, const uint8_t *__restrict__ s0, const uint8_t *__restrict__ c1, const uint8_t *__restrict__ s1,
-                  int kblocks, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+                  int inner, int groups, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t tile = blockIdx.x;                  // (row tile, k block), k block fastest
-    const int64_t rt = tile / kblocks;
-    const int kb = (int)(tile - rt * kblocks);
+    const int64_t tile = blockIdx.x;
+    const int half = GATE_UP ? (int)(tile & 1) : 0;
+    const int64_t q = GATE_UP ? tile >> 1 : tile, g = q / inner;
+    const int at = (int)(q - g * inner);
+    auto source = [&](int r) {      // of row r: in blocks of 128 columns
+        return GATE_UP ? (g * 128 + half * 64 + (r & 63)) * inner + at : ((int64_t)at * 128 + r) * groups + g;
+    };
     for (int i = threadIdx.x; i < 512; i += 256) {    // 128 rows x 4 chunks of 16 bytes
         const int r = i >> 2;
-        const bool second = c1 != nullptr && r >= 64;
-        const int64_t row = c1 == nullptr ? rt * 128 + r : rt * 64 + (r & 63);
-        const uint8_t *src = (second ? c1 : c0) + (row * kblocks + kb) * 64;
+        const uint8_t *src = (GATE_UP && r >= 64 ? c1 : c0) + source(r) * 64;
         reinterpret_cast<uint4 *>(codes + tile * 8192)[i] = reinterpret_cast<const uint4 *>(src)[i & 3];
     }
     if (threadIdx.x < 128) {
         const int r = threadIdx.x;
-        const bool second = c1 != nullptr && r >= 64;
-        const int64_t row = c1 == nullptr ? rt * 128 + r : rt * 64 + (r & 63);
-        const uint32_t v = reinterpret_cast<const uint32_t *>(second ? s1 : s0)[row * kblocks + kb];
+        const uint32_t v = reinterpret_cast<const uint32_t *>(GATE_UP && r >= 64 ? s1 : s0)[source(r)];
         reinterpret_cast<uint32_t *>(scales + tile * kMxTileBytes)[(r & 31) * 4 + (r >> 5)] = v;
     }
 }
@@ -283,10 +284,11 @@ cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_
         return CS_ERR_UNSUPPORTED;
     const int dk = plan->cfg.d / 128, G = plan->G;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_pdl(true, pack_tiles_kernel, dim3(2 * G * dk), dim3(256), 0, st, gate->codes, gate->scales, up->codes, up->scales, dk,
+    cudaError_t e = launch_pdl(true, pack_tiles_kernel<true>, dim3(2 * G * dk), dim3(256), 0, st, gate->codes, gate->scales, up->codes, up->scales, dk, G,
                                gate_up_codes, gate_up_scales);
     if (e == cudaSuccess)
-        e = launch_pdl(true, pack_tiles_kernel, dim3(dk * G), dim3(256), 0, st, down->codes, down->scales, nullptr, nullptr, G, down_codes, down_scales);
+        e = launch_pdl(true, pack_tiles_kernel<false>, dim3(dk * G), dim3(256), 0, st, down->codes, down->scales, nullptr, nullptr, dk, G, down_codes,
+                       down_scales);
     return status_of(e);
 }
 

@@ -157,27 +157,17 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             for (int i = pair; i < items; i += pairs) {
                 const WideItem t = wide_item<DOWN>(w, count, i);
                 const int kb = p.d >> 7;
-                // tiles of 128 rows: gate/up's two halves of a group; the output's 128-column tiles, of which the last may be missing
-                const int row0 = DOWN ? t.col + (int)rank * rows : 0;
-                const int tile0 = DOWN ? t.col >> 7 : 2 * bars.list[t.col];
-                const int tile1 = DOWN ? min(tile0 + 1, kb - 1) : tile0 + 1;
+                // Gate/up: this CTA's half of the group.  Down: `rows` rows of W_down from where they stand, which may run into the next group's (columns
+                // behind d, left out later); two tiles of scales from the one that holds the first column.
                 for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
                     if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
                     uint8_t *st = smem + ring.stage * kWideStageBytes + 128 * 128;
                     const uint32_t full = full0 + 8u * ring.stage;
-                    const int pitch = DOWN ? p.G : kb, at = DOWN ? bars.list[j] : j;
-                    if (BLOCKS == 4) {
-                        tma_load_2d_pair(st, &tm_w, 0, ((rank ? tile1 : tile0) * pitch + at) * 128, full);
-                    } else {
-                        for (int b = 0; b < 3; ++b) {      // 96 rows from wherever they stand, 32 at a time
-                            const int row = row0 + 32 * b;
-                            tma_load_2d_pair(st + 32 * 128 * b, &tm_w, 0, (min(row >> 7, kb - 1) * pitch + at) * 128 + (row & 127), full);
-                        }
-                    }
-                    tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, &tm_ws, 0, tile0 * pitch + at, full);
-                    tma_load_2d_pair(st + kMxWBytes + 2 * kMxTileBytes, &tm_ws, 0, tile1 * pitch + at, full);
+                    const int tile = DOWN ? bars.list[j] * kb + (t.col >> 7) : (bars.list[t.col] * kb + j) * 2;
+                    tma_load_2d_pair(st, &tm_w, 0, tile * 128 + (DOWN ? (t.col & 127) : 0) + (int)rank * rows, full);
+                    tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, &tm_ws, 0, tile, full);
                     if (!DOWN && fill >= kWideStages && ahead < kb * count) {      // the down product's weights on their way to L2
-                        const size_t tile = (size_t)(ahead / count) * p.G + bars.list[ahead % count];
+                        const size_t tile = (size_t)bars.list[ahead / kb] * kb + ahead % kb;
                         prefetch_l2(w.down_codes + tile * kMxWLoad, kMxWLoad);
                         prefetch_l2(w.down_scales + tile * kMxTileBytes, kMxTileBytes);
                         ahead += gridDim.x;
@@ -350,12 +340,12 @@ mx_wide_sum_kernel(const WideArgs w) {
     *reinterpret_cast<uint2 *>(w.p.out + (size_t)t * w.p.d + c) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
 }
 
-// Tiles of 512 scales, one box each.
-bool make_map_scales(CUtensorMap *map, const void *base, uint64_t tiles) {
+// Tiles of 512 scales, `box_tiles` to a box.
+bool make_map_scales(CUtensorMap *map, const void *base, uint64_t tiles, uint32_t box_tiles) {
     EncodeTiledFn fn = encode_fn();
     if (fn == nullptr) return false;
     const cuuint64_t dims[2] = {128, tiles}, strides[1] = {kMxTileBytes};
-    const cuuint32_t box[2] = {128, 1}, estr[2] = {1, 1};
+    const cuuint32_t box[2] = {128, box_tiles}, estr[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -404,10 +394,10 @@ cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, 
     // Fewer items than pairs: cut the list, into parts of at least four k blocks
     if (2 * items <= pairs) w.splits = max(1, min(min(pairs / items, 8), args.cap / 4));
     CUtensorMap x, xs, wg, wgs, a, as, wd, wds;
-    if (!make_map_bytes(&x, q, args.d, B, 128) || !make_map_scales(&xs, args.x_scales, (uint64_t)chunks * kb) ||
-        !make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb, 128) || !make_map_scales(&wgs, L->gate_up_scales, (uint64_t)2 * G * kb) ||
-        !make_map_bytes(&a, plan->mx_a, (uint64_t)args.cap * 128, B, 128) || !make_map_scales(&as, plan->mx_a_scales, (uint64_t)chunks * args.cap) ||
-        !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G, w.width == 256 ? 128 : 32) || !make_map_scales(&wds, L->down_scales, (uint64_t)kb * G)) {
+    if (!make_map_bytes(&x, q, args.d, B, 128) || !make_map_scales(&xs, args.x_scales, (uint64_t)chunks * kb, 1) ||
+        !make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb, 128) || !make_map_scales(&wgs, L->gate_up_scales, (uint64_t)2 * G * kb, 2) ||
+        !make_map_bytes(&a, plan->mx_a, (uint64_t)args.cap * 128, B, 128) || !make_map_scales(&as, plan->mx_a_scales, (uint64_t)chunks * args.cap, 1) ||
+        !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G, w.width / 2) || !make_map_scales(&wds, L->down_scales, (uint64_t)kb * G, 2)) {
         snprintf(plan->cuda_error, sizeof plan->cuda_error, "cuTensorMapEncodeTiled failed");
         return CS_ERR_CUDA;
     }
