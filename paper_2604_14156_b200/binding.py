@@ -511,22 +511,25 @@ def cs_ffn_exec_shared(plan: Plan, layer: Layer, H, support, out=None, stream=No
 
 # ---- microscaled low precision ---------------------------------------------------------------------
 
-_BYTES = (torch.uint8, torch.float8_e8m0fnu, torch.float8_e4m3fn)
+_E8M0, _E4M3 = torch.float8_e8m0fnu, torch.float8_e4m3fn
+_BYTES = (torch.uint8, _E8M0, _E4M3)
 
 
-def _on_current_device(*tensors):
-    """The calls enqueue on the current device's stream: a tensor of another device must not reach them."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != device:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{device}")
+def _device_index() -> int:
+    return _current_device() if _current_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
-def _byte_ptr(t: torch.Tensor, name: str, shape) -> int:
-    """A tensor of one-byte elements (uint8, or the float8 type they are): the pointer."""
-    if t.dtype not in _BYTES:
-        raise TypeError(f"{name} must hold bytes (uint8, float8_e8m0fnu or float8_e4m3fn), got {t.dtype}")
-    return _ptr(t, t.dtype, name, shape)
+def _checked(t, dtypes, name: str, shape, device: int, optional: bool = False) -> Optional[int]:
+    """The pointer of a contiguous tensor of one of `dtypes` and of this shape on the device whose stream the call uses.  The usual case
+    is one line (half a microsecond a tensor is most of what a small call takes on the host)."""
+    if t is None and optional:
+        return None
+    if t.dtype in dtypes and t.get_device() == device and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(map(str, dtypes))}, got {t.dtype}")
+    _ptr(t, t.dtype, name, shape)
+    raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
 
 
 def _dtype_code(t: torch.Tensor, name: str) -> int:
@@ -535,25 +538,58 @@ def _dtype_code(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
+def _outputs(templates, key, device, *specs):
+    """Templates of (shape, dtype) outputs under `key`, to be passed to torch.empty_like: half the host time of naming shape, type and device, as in
+    Plan.outputs (one element each, strides 0; none is kept from a graph capture, whose memory pool it would keep alive)."""
+    t = templates.get(key)
+    if t is None:
+        t = tuple(torch.empty_strided(shape, (0,) * len(shape), dtype=dtype, device=device) for shape, dtype in specs)
+        if not (device.type == "cuda" and torch.cuda.is_current_stream_capturing()):
+            if len(templates) >= 64:
+                templates.clear()
+            templates[key] = t
+    return t
+
+
+_empty_like = torch.empty_like
+_matrix_templates = {}
+
+
+def _matrix(t, dtypes, name: str, device: int):
+    """(pointer, row stride) of a CUDA matrix with contiguous rows."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA matrix")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(map(str, dtypes))}, got {t.dtype}")
+    rows, cols = t.shape
+    if rows == 0 or cols == 0:
+        raise ValueError(f"{name} is empty")
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
+    return t.data_ptr(), (ld if rows > 1 else cols)
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
 def cs_mx_quantize(w, transpose: bool = False, codes=None, scales=None, stream=None):
     """w [rows, cols] f32 or bf16, rows contiguous (any row stride) -> (codes [rows, 16 ceil(cols/32)] uint8, scales
     [rows, ceil(cols/32)] float8_e8m0fnu): blocks of 32 four-bit elements.  transpose: those of the transpose (Wd_t ->
     W_down)."""
-    lib = load_library()
-    if w.dim() != 2 or not w.is_cuda:
-        raise TypeError("w must be a CUDA matrix")
+    lib = _lib or load_library()
+    device = _device_index()
+    ptr, ld = _matrix(w, _FLOATS, "w", device)
     rows, cols = w.shape
-    if rows == 0 or cols == 0:
-        raise ValueError("w is empty")
-    if cols > 1 and w.stride(1) != 1:
-        raise ValueError("w must have contiguous rows")
-    ld = w.stride(0) if rows > 1 else cols
     n, nb = (cols, -(-rows // 32)) if transpose else (rows, -(-cols // 32))
-    codes = torch.empty((n, 16 * nb), dtype=torch.uint8, device=w.device) if codes is None else codes
-    scales = torch.empty((n, nb), dtype=torch.float8_e8m0fnu, device=w.device) if scales is None else scales
-    _on_current_device(w, codes, scales)
-    st = lib.cs_mx_quantize(w.data_ptr(), _dtype_code(w, "w"), rows, cols, ld, int(bool(transpose)),
-                            _ptr(codes, torch.uint8, "codes", (n, 16 * nb)), _byte_ptr(scales, "scales", (n, nb)), _stream(stream))
+    t = _outputs(_matrix_templates, (n, nb, device), w.device, ((n, 16 * nb), torch.uint8), ((n, nb), _E8M0))
+    codes = _empty_like(t[0]) if codes is None else codes
+    scales = _empty_like(t[1]) if scales is None else scales
+    st = lib.cs_mx_quantize(ptr, _DTYPES[w.dtype], rows, cols, ld, 1 if transpose else 0,
+                            _checked(codes, (torch.uint8,), "codes", (n, 16 * nb), device),
+                            _checked(scales, _BYTES, "scales", (n, nb), device), _stream(stream))
     if st != 0:
         raise CSError(st, "cs_mx_quantize")
     return codes, scales
@@ -561,16 +597,17 @@ def cs_mx_quantize(w, transpose: bool = False, codes=None, scales=None, stream=N
 
 def cs_mx_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, stream=None):
     """The values [rows, cols] of cs_mx_quantize's codes and scales, as f32 or bf16."""
-    lib = load_library()
-    if codes.dim() != 2:
-        raise ValueError("codes must be a matrix")
+    lib = _lib or load_library()
+    device = _device_index()
     rows, nb = codes.shape[0], -(-cols // 32)
-    out = torch.empty((rows, cols), dtype=dtype, device=codes.device) if out is None else out
-    if tuple(out.shape) != (rows, cols) or not out.is_cuda or (cols > 1 and out.stride(1) != 1):
-        raise ValueError(f"out must be a CUDA matrix of shape ({rows}, {cols}) with contiguous rows")
-    _on_current_device(codes, scales, out)
-    st = lib.cs_mx_dequantize(_ptr(codes, torch.uint8, "codes", (rows, 16 * nb)), _byte_ptr(scales, "scales", (rows, nb)), rows, cols,
-                              _dtype_code(out, "out"), out.data_ptr(), out.stride(0) if rows > 1 else cols, _stream(stream))
+    if out is None:
+        out = _empty_like(_outputs(_matrix_templates, (rows, cols, dtype, device), codes.device, ((rows, cols), dtype))[0])
+    ptr, ld = _matrix(out, _FLOATS, "out", device)
+    if out.shape != (rows, cols):
+        raise ValueError(f"out must have shape {(rows, cols)}, got {tuple(out.shape)}")
+    st = lib.cs_mx_dequantize(_checked(codes, (torch.uint8,), "codes", (rows, 16 * nb), device),
+                              _checked(scales, _BYTES, "scales", (rows, nb), device), rows, cols, _DTYPES[out.dtype], ptr, ld,
+                              _stream(stream))
     if st != 0:
         raise CSError(st, "cs_mx_dequantize")
     return out
@@ -582,11 +619,11 @@ class MxLayer:
 
     def __init__(self, plan: Plan, gate, up, down, stream=None):
         d, d_ff = plan.d, plan.d_ff
+        device = _device_index()
 
         def matrix(pair, name, rows, cols):
-            return _MxMatrix(_ptr(pair[0], torch.uint8, name + " codes", (rows, cols // 2)),
-                             _byte_ptr(pair[1], name + " scales", (rows, cols // 32)))
-        _on_current_device(*gate, *up, *down)
+            return _MxMatrix(_checked(pair[0], (torch.uint8,), name + " codes", (rows, cols // 2), device),
+                             _checked(pair[1], _BYTES, name + " scales", (rows, cols // 32), device))
         ms = matrix(gate, "gate", d_ff, d), matrix(up, "up", d_ff, d), matrix(down, "down", d, d_ff)
         n = d * d_ff
         self.tensors = tuple(torch.empty((size,), dtype=torch.uint8, device=gate[0].device) for size in (n, n // 16, n // 2, n // 32))
@@ -600,29 +637,43 @@ def cs_mx_norm(plan: Plan, x, gamma=None, delta=None, want_n: bool = False, x_ou
     """h = x + delta, n = RMSNorm(h) * gamma, in blocks of 32 e4m3 elements.  Returns (h, q [B, d] float8_e4m3fn, s
     [ceil(B/128), d/128, 32, 4, 4] float8_e8m0fnu, n or None); h is x itself without a delta and x_out.  s is in tile order: the scale
     of row r, block b stands at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4]."""
-    B, d = x.shape[0], plan.d
-    dev = x.device
-    _on_current_device(x, delta, gamma, x_out)
-    if x_out is None and delta is not None:
-        x_out = torch.empty_like(x)
-    n = torch.empty((B, d), dtype=torch.float32, device=dev) if want_n else None
-    q = torch.empty((B, d), dtype=torch.float8_e4m3fn, device=dev)
-    s = torch.empty((-(-B // 128), d // 128, 32, 4, 4), dtype=torch.float8_e8m0fnu, device=dev)
-    code = _dtype_code(x, "x")
-    plan.check(plan.lib.cs_mx_norm(plan.handle, _ptr(x, x.dtype, "x", (B, d)), code,
-                                   None if delta is None else _ptr(delta, delta.dtype, "delta", (B, d)),
-                                   0 if delta is None else _dtype_code(delta, "delta"),
-                                   _ptr(gamma, torch.float32, "gamma", (d,)), B, _ptr(x_out, x.dtype, "x_out", (B, d)),
-                                   None if n is None else n.data_ptr(), q.data_ptr(), s.data_ptr(), _stream(stream)), "cs_mx_norm")
-    return (x if x_out is None else x_out), q, s, n
+    B, d, dev = x.shape[0], plan.d, x.device
+    rows = (B, d)
+    device = _device_index()
+    px = _checked(x, _FLOATS, "x", rows, device)
+    pd = _checked(delta, _FLOATS, "delta", rows, device, True)
+    pg = _checked(gamma, (torch.float32,), "gamma", (d,), device, True)
+    if x_out is None:
+        if delta is not None:
+            x_out = torch.empty_like(x)
+            po = x_out.data_ptr()
+        else:
+            x_out, po = x, None
+    else:
+        po = _checked(x_out, (x.dtype,), "x_out", rows, device)
+    t = _outputs(plan._templates, ("norm", B, device), dev, (rows, torch.float32), (rows, _E4M3), ((-(-B // 128), d // 128, 32, 4, 4), _E8M0))
+    n = _empty_like(t[0]) if want_n else None
+    q, s = _empty_like(t[1]), _empty_like(t[2])
+    st = plan.lib.cs_mx_norm(plan.handle, px, _DTYPES[x.dtype], pd, 0 if pd is None else _DTYPES[delta.dtype], pg, B, po,
+                             None if n is None else n.data_ptr(), q.data_ptr(), s.data_ptr(), _stream(stream))
+    if st != 0:
+        plan.check(st, "cs_mx_norm")
+    return x_out, q, s, n
 
 
 def _mx_ffn(call, name, plan: Plan, layer: MxLayer, q, s, support, support_shape, out, stream):
     B, d = q.shape[0], plan.d
-    out = torch.empty((B, d), dtype=torch.bfloat16, device=q.device) if out is None else out
-    _on_current_device(q, s, support, out)
-    plan.check(call(plan.handle, layer.ref, _byte_ptr(q, "q", (B, d)), _byte_ptr(s, "s", (-(-B // 128), d // 128, 32, 4, 4)),
-                    _ptr(support, torch.int32, "support", support_shape), B, _ptr(out, torch.bfloat16, "out", (B, d)), _stream(stream)), name)
+    device = _device_index()
+    if out is None:
+        out = _empty_like(_outputs(plan._templates, ("ffn", B, device), q.device, ((B, d), torch.bfloat16))[0])
+        po = out.data_ptr()
+    else:
+        po = _checked(out, (torch.bfloat16,), "out", (B, d), device)
+    st = call(plan.handle, layer.ref, _checked(q, _BYTES, "q", (B, d), device),
+              _checked(s, _BYTES, "s", (-(-B // 128), d // 128, 32, 4, 4), device),
+              _checked(support, (torch.int32,), "support", support_shape, device), B, po, _stream(stream))
+    if st != 0:
+        plan.check(st, name)
     return out
 
 

@@ -63,8 +63,11 @@ def test_plan_shapes(kw):
 
 def test_binding_refuses_cpu_and_foreign_types():
     with pytest.raises(TypeError):
-        cs.cs_mx_quantize(torch.zeros(4, 32))
+        binding._matrix(torch.zeros(4, 32), binding._FLOATS, "w", 0)
     with pytest.raises(TypeError):
-        binding._byte_ptr(torch.zeros(4), "q", (4,))
+        binding._checked(torch.zeros(4), binding._BYTES, "q", (4,), 0)
+    with pytest.raises(TypeError):
+        binding._checked(torch.zeros(4, dtype=torch.uint8), binding._BYTES, "q", (4,), 0)
+    assert binding._checked(None, binding._BYTES, "q", (4,), 0, True) is None
     with pytest.raises(TypeError):
         binding._dtype_code(torch.zeros(4, dtype=torch.float16), "x")
