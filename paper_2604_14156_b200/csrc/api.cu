@@ -137,7 +137,7 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
     if (e == cudaSuccess && prepare_prompt(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && prepare_solvers(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && !mx && prepare_ffn_gather(p) != CS_OK) e = cudaErrorUnknown;
-    if (e == cudaSuccess && mx && prepare_mx_ffn(p) != CS_OK) e = cudaErrorUnknown;
+    if (e == cudaSuccess && mx && (prepare_mx_norm() != CS_OK || prepare_mx_ffn(p) != CS_OK)) e = cudaErrorUnknown;
     if (e == cudaSuccess && p->mma_ok && prepare_ffn_mma(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess && p->mma_ok && prepare_decode(p) != CS_OK) e = cudaErrorUnknown;
     if (e == cudaSuccess) e = cudaMemset(p->mask, 0, nt * 4 * sizeof(uint32_t));

@@ -68,6 +68,7 @@ __device__ __forceinline__ float max_abs(float m, float v) {
 }
 
 // mx_norm.cu
+cs_status prepare_mx_norm();
 cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *delta, int delta_dtype, const float *gamma, int B,
                          void *x_out, float *n_out, uint8_t *q, uint8_t *s, cudaStream_t st);
 // mx_ffn.cu: support [B, k], or with `shared` [k]

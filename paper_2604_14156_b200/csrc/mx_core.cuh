@@ -102,6 +102,10 @@ __device__ __forceinline__ bool mx_wait(uint64_t *bar, uint32_t parity, uint32_t
     atomicCAS(&status->code, 0, (int)CS_ERR_TIMEOUT);
     return false;
 }
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
 // Matrix of bytes [rows, inner]: boxes of 128 bytes x box_rows, 128-byte swizzle.
 bool make_map_bytes(CUtensorMap *map, const void *base, uint64_t inner, uint64_t rows, uint32_t box_rows) {
     EncodeTiledFn fn = encode_fn();

@@ -47,10 +47,6 @@ __host__ __device__ inline int mx_tmem_cols(int tile, int stages) {
     return c;
 }
 
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
-}
 // 512 bytes of scales to four tensor-memory columns, repeated in the four lane quarters.
 __device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint32_t saddr) {
     const uint64_t desc = (uint64_t)((saddr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);

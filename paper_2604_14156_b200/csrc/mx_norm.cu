@@ -1,8 +1,10 @@
 // The residual's addition, RMSNorm and the result in blocks of 32 e4m3 elements (mx.cuh), one pass over the row:
 //   h = x + delta (rounded to x's type),  n = h / sqrt(mean(h^2) + eps) * gamma,  q, s = blocks of n.
-// A row is one CTA, eight elements a thread, kept in registers between the sum of squares and the quantisation, so HBM sees every byte
-// once; the sum is held in f32 (eight terms a thread, then a tree).
-#include "mx.cuh"
+// A row is one pass of one CTA, eight elements a thread, kept in registers between the sum of squares and the quantisation, so HBM sees every byte
+// once; the sum is held in f32 (eight terms a thread, then a tree).  mx_norm_kernel is a CTA per row: one round of latencies, for as many rows as are
+// resident at once.  More rows take mx_norm_rows_kernel, whose CTAs stay and have the next rows' bulk copies in flight while they work on one: with a CTA
+// per row the loads wait for the row before (2048 rows of 5120 bf16 took 21.5 us).
+#include "mx_core.cuh"
 
 namespace cs {
 
@@ -30,88 +32,217 @@ template <typename T> __device__ __forceinline__ void store_row8(T *p, const flo
     }
 }
 
-// x_out may be x.  d / 8 threads, rounded up to whole warps.  CTAs behind the last row clear the scales of the rows that its tile of 128 has left over.
-template <typename TX, typename TD> __global__ void __launch_bounds__(1024)
-mx_norm_kernel(const TX *x, const TD *delta, const float *__restrict__ gamma, int B, int d, float eps, TX *x_out, float *n_out, uint8_t *q, uint8_t *s) {
-    __shared__ float part[32];
-    const int kblocks = d >> 7;
-    if ((int)blockIdx.x >= B) {
-        pdl_launch_dependents();
-        pdl_wait();
-        const int quarter = blockIdx.x - B, tile = (B - 1) >> 7;      // 32 rows of the last tile
-        for (int i = threadIdx.x; i < 32 * kblocks; i += blockDim.x) {
-            const int r = i & 31;
-            if (tile * 128 + quarter * 32 + r >= B)
-                reinterpret_cast<uint32_t *>(s + ((size_t)tile * kblocks + (i >> 5)) * kMxTileBytes)[r * 4 + quarter] = 0;
-        }
-        return;
-    }
-    const int t = threadIdx.x, row = blockIdx.x;
-    const bool in = t * 8 < d;
-    const size_t at = (size_t)row * d + t * 8;
-    float g[8], h[8];
+// 1 / sqrt of the mean square plus eps; the approximation is within 2 units in the last place.
+__device__ __forceinline__ float row_scale(float sum, int d, float eps) { return rsqrtf(sum / (float)d + eps); }
+
+// Eight elements of a row, chunk c, once the row's scale is known; `in`: there are any.  Sixteen neighbouring lanes hold sixteen neighbouring chunks.
+__device__ __forceinline__ void finish_chunk(float (&h)[8], const float (&g)[8], float rstd, int d, int row, int c, bool in, float *n_out, uint8_t *q,
+                                             uint8_t *s) {
+    float top = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { g[j] = 1.f; h[j] = 0.f; }
-    if (in && gamma != nullptr) {
-        const float4 a = __ldg(reinterpret_cast<const float4 *>(gamma) + 2 * t), b = __ldg(reinterpret_cast<const float4 *>(gamma) + 2 * t + 1);
-        g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
-    }
-    pdl_launch_dependents();
-    pdl_wait();
-    float sum = 0.f;
-    if (in) {
-        load_row8(x + at, h);
-        if (delta != nullptr) {
-            float a[8];
-            load_row8(delta + at, a);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                h[j] += a[j];
-                if (sizeof(TX) == 2) h[j] = __bfloat162float(__float2bfloat16_rn(h[j]));   // the norm is that of the stored residual
-            }
-        }
-        if (x_out != nullptr) store_row8(x_out + at, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
-    }
-    sum = warp_sum(sum);
-    const int warps = blockDim.x >> 5;
-    if ((t & 31) == 0) part[t >> 5] = sum;
-    __syncthreads();
-    sum = warp_sum((t & 31) < warps ? part[t & 31] : 0.f);
-    const float rstd = 1.f / sqrtf(sum / (float)d + eps);
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { h[j] = h[j] * rstd * g[j]; m = max(m, abs_bits(h[j])); }
+    for (int j = 0; j < 8; ++j) { h[j] = h[j] * rstd * g[j]; top = max_abs(top, h[j]); }
+    uint32_t m = __float_as_uint(top);
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
     const uint32_t byte = mx_scale_byte<true>(m);
     const float inv = mx_inverse(byte);
     // the four scales of 128 columns are one word of the tile
-    uint32_t word = byte << (8 * ((t >> 2) & 3));
+    uint32_t word = byte << (8 * ((c >> 2) & 3));
     word |= __shfl_xor_sync(0xffffffffu, word, 4);
     word |= __shfl_xor_sync(0xffffffffu, word, 8);
     if (!in) return;
+    const size_t at = (size_t)row * d + c * 8;
     if (n_out != nullptr) store_row8(n_out + at, h);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = byte == 255 ? 0.f : h[j] * inv;
-    *reinterpret_cast<uint2 *>(q + at) = make_uint2(pack_e4m3(h[0], h[1], h[2], h[3]), pack_e4m3(h[4], h[5], h[6], h[7]));
-    if ((t & 15) == 0)
-        reinterpret_cast<uint32_t *>(s + ((size_t)(row >> 7) * kblocks + (t >> 4)) * kMxTileBytes)[(row & 31) * 4 + ((row & 127) >> 5)] = word;
+    for (int j = 0; j < 8; ++j) h[j] *= inv;
+    uint2 v = make_uint2(pack_e4m3(h[0], h[1], h[2], h[3]), pack_e4m3(h[4], h[5], h[6], h[7]));
+    if (byte == 255) v = make_uint2(0, 0);
+    *reinterpret_cast<uint2 *>(q + at) = v;
+    if ((c & 15) == 0)
+        reinterpret_cast<uint32_t *>(s + ((size_t)(row >> 7) * (d >> 7) + (c >> 4)) * kMxTileBytes)[(row & 31) * 4 + ((row & 127) >> 5)] = word;
+}
+// h += delta, rounded to the residual's type: the norm is that of the stored residual.
+template <typename TX> __device__ __forceinline__ void add_delta(float (&h)[8], const float (&a)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        h[j] += a[j];
+        if (sizeof(TX) == 2) h[j] = __bfloat162float(__float2bfloat16_rn(h[j]));
+    }
+}
+__device__ __forceinline__ float squares(const float (&h)[8]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
+    return sum;
+}
+__device__ __forceinline__ void load_gamma(const float *gamma, int t, bool in, float (&g)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = 1.f;
+    if (in && gamma != nullptr) {
+        const float4 a = __ldg(reinterpret_cast<const float4 *>(gamma) + 2 * t), b = __ldg(reinterpret_cast<const float4 *>(gamma) + 2 * t + 1);
+        g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+    }
+}
+// A quarter (32 rows) of the last tile of scales: zeros in the rows from B on.
+__device__ __forceinline__ void clear_scales(uint8_t *s, int B, int kblocks, int quarter) {
+    const int tile = (B - 1) >> 7;
+    for (int i = threadIdx.x; i < 32 * kblocks; i += blockDim.x) {
+        const int r = i & 31;
+        if (tile * 128 + quarter * 32 + r >= B)
+            reinterpret_cast<uint32_t *>(s + ((size_t)tile * kblocks + (i >> 5)) * kMxTileBytes)[r * 4 + quarter] = 0;
+    }
+}
+
+// x_out may be x.  d / 8 threads, rounded up to whole warps.  Four CTAs behind the last row clear the scales of rows that its tile of 128 has left over.
+template <typename TX, typename TD> __global__ void __launch_bounds__(1024)
+mx_norm_kernel(const TX *x, const TD *delta, const float *__restrict__ gamma, int B, int d, float eps, TX *x_out, float *n_out, uint8_t *q, uint8_t *s) {
+    __shared__ float part[32];
+    const int t = threadIdx.x, row = blockIdx.x;
+    if (row >= B) {
+        pdl_launch_dependents();
+        pdl_wait();
+        clear_scales(s, B, d >> 7, row - B);
+        return;
+    }
+    const bool in = t * 8 < d;
+    const size_t at = (size_t)row * d + t * 8;
+    float g[8], h[8];
+    load_gamma(gamma, t, in, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = 0.f;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (in) {
+        float a[8];
+        load_row8(x + at, h);
+        if (delta != nullptr) { load_row8(delta + at, a); add_delta<TX>(h, a); }
+        if (x_out != nullptr) store_row8(x_out + at, h);
+    }
+    float sum = warp_sum(squares(h));
+    if ((t & 31) == 0) part[t >> 5] = sum;
+    __syncthreads();
+    sum = warp_sum((t & 31) < (int)(blockDim.x >> 5) ? part[t & 31] : 0.f);
+    finish_chunk(h, g, row_scale(sum, d, eps), d, row, t, in, n_out, q, s);
+}
+
+constexpr int kNormStages = 8;
+struct NormBars {
+    uint64_t full[kNormStages];
+    uint32_t aborted;
+    float part[2][32];
+};
+template <typename T> __device__ __forceinline__ void read_row8(const uint8_t *p, float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        Chunk<__nv_bfloat16>::widen(*reinterpret_cast<const uint4 *>(p), v);
+    } else {
+        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+}
+
+// Persistent CTAs: CTA c takes rows c, c + gridDim.x, ...; `stages` rows of x (and delta) are in flight or at work in shared memory.  The barrier of a row's
+// sum comes after every thread has read the row, so it also frees the row's place.  E chunks of eight elements a thread, d / (8 E) apart: a row's chain
+// of latencies (load, sum, two reductions, stores) is what there is to hide, with four small CTAs on an SM better than with two large ones.
+template <typename TX, typename TD, int E> __global__ void __launch_bounds__(1024 / E, E == 2 ? 3 : 1)
+mx_norm_rows_kernel(const TX *x, const TD *delta, const float *__restrict__ gamma, int B, int d, float eps, TX *x_out, float *n_out, uint8_t *q, uint8_t *s,
+                    int stages, DeviceStatus *status) {
+    extern __shared__ __align__(128) uint8_t ring_rows[];
+    __shared__ NormBars bars;
+    const int t = threadIdx.x, step = gridDim.x, apart = d / (8 * E);
+    const bool in = t < apart;
+    const uint32_t xb = d * sizeof(TX), db = delta != nullptr ? d * sizeof(TD) : 0, bytes = xb + db;
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(&bars.full[i], 1);
+        bars.aborted = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    pdl_launch_dependents();
+    pdl_wait();
+    auto fetch = [&](int row, int stage) {
+        uint8_t *to = ring_rows + stage * bytes;
+        mbar_expect_tx(&bars.full[stage], bytes);
+        bulk_load(to, x + (size_t)row * d, xb, &bars.full[stage]);
+        if (db != 0) bulk_load(to + xb, delta + (size_t)row * d, db, &bars.full[stage]);
+    };
+    if (t == 0)
+        for (int i = 0, row = blockIdx.x; i < stages && row < B; ++i, row += step) fetch(row, i);
+    if (B % 128 != 0 && (int)blockIdx.x < 4) clear_scales(s, B, d >> 7, blockIdx.x);
+    MxRing ring;
+    int turn = 0;
+    for (int row = blockIdx.x; row < B; row += step, turn ^= 1) {
+        const bool ok = mx_wait(&bars.full[ring.stage], ring.phase, &bars.aborted, status);
+        const uint8_t *from = ring_rows + ring.stage * bytes;
+        float h[E][8], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[e][j] = 0.f;
+            if (ok && in) {
+                const int c = t + e * apart;
+                float a[8];
+                read_row8<TX>(from + c * 8 * sizeof(TX), h[e]);
+                if (db != 0) { read_row8<TD>(from + xb + c * 8 * sizeof(TD), a); add_delta<TX>(h[e], a); }
+            }
+            sum += squares(h[e]);
+        }
+        sum = warp_sum(sum);
+        if ((t & 31) == 0) bars.part[turn][t >> 5] = sum;
+        if (!__syncthreads_and(ok)) return;      // a wait gave up: the status word says so
+        if (t == 0 && row + stages * step < B) fetch(row + stages * step, ring.stage);
+        if (x_out != nullptr && in)
+#pragma unroll
+            for (int e = 0; e < E; ++e) store_row8(x_out + (size_t)row * d + (t + e * apart) * 8, h[e]);
+        sum = warp_sum((t & 31) < (int)(blockDim.x >> 5) ? bars.part[turn][t & 31] : 0.f);
+        const float rstd = row_scale(sum, d, eps);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            float g[8];
+            load_gamma(gamma, t + e * apart, in, g);
+            finish_chunk(h[e], g, rstd, d, row, t + e * apart, in, n_out, q, s);
+        }
+        ring.next(stages);
+    }
+}
+
+constexpr int kNormRings = 208 * 1024;      // an SM's, over its CTAs
+
+template <typename TX, typename TD> cs_status prepare_rows() {
+    for (auto *k : {mx_norm_rows_kernel<TX, TD, 1>, mx_norm_rows_kernel<TX, TD, 2>})
+        if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormRings) != cudaSuccess || prefer_shared(k) != cudaSuccess)
+            return CS_ERR_CUDA;
+    return CS_OK;
 }
 
 }  // namespace
 
+cs_status prepare_mx_norm() {
+    for (cs_status s : {prepare_rows<float, float>(), prepare_rows<float, __nv_bfloat16>(), prepare_rows<__nv_bfloat16, float>(),
+                        prepare_rows<__nv_bfloat16, __nv_bfloat16>()})
+        if (s != CS_OK) return s;
+    return CS_OK;
+}
+
 cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *delta, int delta_dtype, const float *gamma, int B,
                          void *x_out, float *n_out, uint8_t *q, uint8_t *s, cudaStream_t st) {
     const int d = plan->cfg.d;
-    const dim3 grid(B + (B % 128 != 0 ? 4 : 0)), block((d / 8 + 31) / 32 * 32);
+    const dim3 block((d / 8 + 31) / 32 * 32);
+    // One CTA per row while all of them are resident at once.  Beyond, CTAs that stay: as many to an SM as leave each two rows of ring.
+    const bool stay = B > plan->sm_count * (2048 / (int)block.x);
+    const int row_bytes = d * ((x_dtype == CS_F32 ? 4 : 2) + (delta == nullptr ? 0 : delta_dtype == CS_F32 ? 4 : 2));
+    const int each = d % 256 == 0 ? 2 : 1, threads = (d / (8 * each) + 31) / 32 * 32;
+    const int ctas = max(1, min(min(4, 1280 / threads), kNormRings / (2 * row_bytes))), stages = min(kNormStages, kNormRings / ctas / row_bytes);
     cudaError_t e;
     auto go = [&](auto tx, auto td) {
         using TX = decltype(tx);
         using TD = decltype(td);
-        e = launch_pdl(true, mx_norm_kernel<TX, TD>, grid, block, 0, st, static_cast<const TX *>(x), static_cast<const TD *>(delta), gamma, B, d,
-                       plan->cfg.rms_eps, static_cast<TX *>(x_out), n_out, q, s);
+        if (stay)
+            e = launch_pdl(true, each == 2 ? mx_norm_rows_kernel<TX, TD, 2> : mx_norm_rows_kernel<TX, TD, 1>, dim3(ctas * plan->sm_count), dim3(threads),
+                           (size_t)stages * row_bytes, st, static_cast<const TX *>(x), static_cast<const TD *>(delta), gamma, B, d, plan->cfg.rms_eps,
+                           static_cast<TX *>(x_out), n_out, q, s, stages, plan->status);
+        else
+            e = launch_pdl(true, mx_norm_kernel<TX, TD>, dim3(B + (B % 128 != 0 ? 4 : 0)), block, 0, st, static_cast<const TX *>(x),
+                           static_cast<const TD *>(delta), gamma, B, d, plan->cfg.rms_eps, static_cast<TX *>(x_out), n_out, q, s);
     };
     if (x_dtype == CS_F32) {
         if (delta_dtype == CS_F32) go(0.f, 0.f); else go(0.f, __nv_bfloat16());
