@@ -26,6 +26,7 @@ constexpr int kMxThreads = 128 + 32 * kMxEpiWarps;   // weight loads, MMA, token
 constexpr int kMxMaxTile = 256;                      // tokens of a tile
 constexpr int kMxMaxStages = 8;
 constexpr int kMxMaxCluster = 8;
+constexpr int kMxPitch = 132;                        // floats from column to column of the spilled tile: float4 reads of 8 columns hit all banks
 constexpr int kMxNarrowTokens = 128;                 // larger batches take the pairs of mx_wide.cu
 
 struct MxBars {
@@ -62,11 +63,6 @@ __device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t a, uint64_t b, ui
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
 }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kMxEpiWarps) : "memory"); }
-__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -180,7 +176,7 @@ __device__ __forceinline__ void mx_products(const MxArgs &p, uint8_t *smem, MxBa
     }
     if (r.n > 0) tc_commit(&bars->acc);
 }
-// The accumulators of the tile's valid tokens to shared memory, [column][128 rows], over the drained ring; zeros where there was no k block.
+// The accumulators of the tile's valid tokens to shared memory, [column][kMxPitch], over the drained ring; zeros where there was no k block.
 __device__ __forceinline__ void mx_spill(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int valid) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
     float *tile = reinterpret_cast<float *>(smem) + quarter * 32 + lane;
@@ -191,8 +187,21 @@ __device__ __forceinline__ void mx_spill(const MxArgs &p, uint8_t *smem, MxBars 
         if (ok) { tc_ld16(bars->tmem + ((uint32_t)quarter << 21) + c, v); tc_wait_ld(); }
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (c + j < valid) tile[(c + j) * 128] = ok ? __uint_as_float(v[j]) : 0.f;
+            if (c + j < valid) tile[(c + j) * kMxPitch] = ok ? __uint_as_float(v[j]) : 0.f;
     }
+}
+
+// Four floats at this shared-memory offset in each of the cluster's CTAs, added in rank order; all loads are in flight together.
+__device__ __forceinline__ float4 sum_ranks(uint32_t addr, int cs) {
+    float4 u[kMxMaxCluster];
+#pragma unroll
+    for (int q = 0; q < kMxMaxCluster; ++q)
+        if (q < cs) u[q] = ld_cluster4(map_to_cta(addr, q));
+    float4 v = u[0];
+#pragma unroll
+    for (int q = 1; q < kMxMaxCluster; ++q)
+        if (q < cs) { v.x += u[q].x; v.y += u[q].y; v.z += u[q].z; v.w += u[q].w; }
+    return v;
 }
 
 __device__ __forceinline__ uint8_t *mx_setup(MxBars *bars, int stages, int cols, const CUtensorMap *a, const CUtensorMap *b) {
@@ -273,36 +282,41 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
         __syncwarp();
         if (cs > 1) cluster_sync_all();
         if (warp >= 4) {
-            if (cs == 1) epilogue_sync();
-            // a column to a warp, two neighbouring channels to a lane: lanes 0..15 hold one block of 32, lanes 16..31 the other
-            const uint32_t base = smem_u32(smem) + lane * 8;
-#pragma unroll 2
-            for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
-                const int t = z * p.tile + c;
-                float g0 = 0.f, g1 = 0.f, u0 = 0.f, u1 = 0.f;
-                if (cs == 1) {
-                    const float2 *row = reinterpret_cast<const float2 *>(smem + (size_t)c * 512) + lane;
-                    g0 = row[0].x; g1 = row[0].y; u0 = row[32].x; u1 = row[32].y;
-                } else {
-                    for (int q = 0; q < cs; ++q) {
-                        const uint32_t peer = map_to_cta(base + c * 512, q);
-                        const float2 a = ld_cluster2(peer), b = ld_cluster2(peer + 256);
-                        g0 += a.x; g1 += a.y; u0 += b.x; u1 += b.y;
-                    }
+            if (cs > 1)      // this CTA's columns, every cs-th, summed in place: no other CTA reads them
+                for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
+                    const uint32_t at = (uint32_t)(c * kMxPitch + lane * 4) * 4;
+                    *reinterpret_cast<float4 *>(smem + at) = sum_ranks(smem_u32(smem) + at, cs);
                 }
-                const bool member = p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1);
-                float a0 = member ? swiglu(g0, u0) : 0.f, a1 = member ? swiglu(g1, u1) : 0.f;
-                uint32_t m = max(abs_bits(a0), abs_bits(a1));
+            epilogue_sync();
+            // four threads to a column, sixteen channels each: a block of 32 is two neighbours'
+            for (int i = threadIdx.x - 128;; i += 32 * kMxEpiWarps) {
+                const int c = (i >> 2) * cs + rank, part = i & 3, t = z * p.tile + c;
+                if (__all_sync(0xffffffffu, c >= valid)) break;
+                const bool in = c < valid;
+                const bool member = in && (p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1));
+                const float4 *gate = reinterpret_cast<const float4 *>(smem) + (in ? c * (kMxPitch / 4) : 0) + part * 4, *up = gate + 16;
+                float a[16], m = 0.f;
 #pragma unroll
-                for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const uint32_t byte = mx_scale_byte<true>(m);
+                for (int j = 0; j < 4; ++j) {
+                    const float4 x = gate[j], y = up[j];
+                    a[4 * j] = swiglu(x.x, y.x); a[4 * j + 1] = swiglu(x.y, y.y); a[4 * j + 2] = swiglu(x.z, y.z); a[4 * j + 3] = swiglu(x.w, y.w);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) m = max_abs(m, a[j]);
+                m = max_abs(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                const uint32_t byte = member ? mx_scale_byte<true>(__float_as_uint(m)) : 0u;
                 const float inv = mx_inverse(byte);
-                a0 = byte == 255 ? 0.f : a0 * inv; a1 = byte == 255 ? 0.f : a1 * inv;
-                reinterpret_cast<uint16_t *>(p.a + (size_t)t * p.cap * 128 + entry * 128 + half * 64)[lane] = pack_e4m3x2(a0, a1);
-                const uint32_t other = __shfl_down_sync(0xffffffffu, byte, 16);
-                if (lane == 0)
-                    *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(t >> 7) * p.cap + entry) * kMxTileBytes + (t & 31) * 16 + ((t & 127) >> 5) * 4 + half * 2) =
-                        (uint16_t)(byte | other << 8);
+                uint32_t o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = !member || byte == 255 ? 0u : pack_e4m3(a[4 * j] * inv, a[4 * j + 1] * inv, a[4 * j + 2] * inv, a[4 * j + 3] * inv);
+                const uint32_t other = __shfl_down_sync(0xffffffffu, byte, 2);
+                if (in) {
+                    *reinterpret_cast<uint4 *>(p.a + (size_t)t * p.cap * 128 + entry * 128 + half * 64 + part * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (part == 0)
+                        *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(t >> 7) * p.cap + entry) * kMxTileBytes + (t & 31) * 16 + ((t & 127) >> 5) * 4 + half * 2) =
+                            (uint16_t)(byte | other << 8);
+                }
             }
         }
         if (cs > 1) cluster_sync_all();      // peers are done with this CTA's tile
@@ -350,18 +364,10 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     if (cs > 1) cluster_sync_all();
     if (warp >= 4) {
         if (cs == 1) epilogue_sync();
-        const uint32_t base = smem_u32(smem) + lane * 16;
 #pragma unroll 2
         for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (cs == 1) {
-                v = *reinterpret_cast<const float4 *>(smem + (size_t)c * 512 + lane * 16);
-            } else {
-                for (int q = 0; q < cs; ++q) {
-                    const float4 u = ld_cluster4(map_to_cta(base + c * 512, q));
-                    v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-                }
-            }
+            const uint32_t at = (uint32_t)(c * kMxPitch + lane * 4) * 4;
+            const float4 v = cs == 1 ? *reinterpret_cast<const float4 *>(smem + at) : sum_ranks(smem_u32(smem) + at, cs);
             const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
             *reinterpret_cast<uint2 *>(p.out + (size_t)(z * p.tile + c) * p.d + blockIdx.y * 128 + lane * 4) =
                 make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
@@ -384,7 +390,9 @@ cudaError_t launch_clusters(void (*kernel)(const CUtensorMap, const CUtensorMap,
     return cudaLaunchKernelEx(&cfg, kernel, w, x, p);
 }
 
-constexpr int kMxSmemOne = 226 * 1024, kMxSmemTwo = 112 * 1024;   // a CTA's shared memory, alone on its SM or with another
+constexpr int kMxBesideTokens = 32;
+constexpr int kMxSmemOne = 226 * 1024, kMxSmemTwo = 112 * 1024;   // a CTA's shared memory, alone on its SM or with another of its kind ...
+constexpr int kMxSmemGateUp = 126 * 1024, kMxSmemDown = 99 * 1024;   // ... or a gate/up CTA's beside a down CTA's
 
 }  // namespace
 
@@ -402,11 +410,13 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int rows = shared ? 1 : B;
     const bool wide = B > kMxNarrowTokens;
     const int tile = min(kMxMaxTile, (B + 15) / 16 * 16), tiles = (B + tile - 1) / tile;
-    const bool two = tile <= 128;                        // two CTAs on an SM
-    const int room = (two ? kMxSmemTwo : kMxSmemOne) - 1024 - (int)sizeof(MxBars) - 64;
-    const int stages = max(2, min(kMxMaxStages, room / mx_stage_bytes(tile)));
-    const size_t smem = 1024 + (size_t)max(stages * mx_stage_bytes(tile), tile * 512);
+    // Shared memory.  Up to 32 tokens one CTA of each product fits on an SM beside the other, so that down's CTAs start, and load their weights, while
+    // gate/up runs; beyond, two CTAs of a product, or one where a tile has more than 128 tokens.
+    const bool beside = tile <= kMxBesideTokens, two = !beside && tile <= 128;
     const int slots = plan->sm_count * (two ? 2 : 1);
+    auto ring = [&](int bytes) { return max(2, min(kMxMaxStages, (bytes - 1024 - (int)sizeof(MxBars) - 64) / mx_stage_bytes(tile))); };
+    const int stages = ring(beside ? kMxSmemGateUp : two ? kMxSmemTwo : kMxSmemOne), down_stages = beside ? ring(kMxSmemDown) : stages;
+    auto smem_of = [&](int n) { return 1024 + (size_t)max(n * mx_stage_bytes(tile), tile * kMxPitch * 4); };
     CUtensorMap wg, wd, xm, am;
     if (!wide && (!make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb) || !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G) ||
         !make_map_bytes(&xm, q, d, B, tile) || !make_map_bytes(&am, plan->mx_a, (uint64_t)cap * 128, B, tile))) {
@@ -427,13 +437,12 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
         plan->launches += 1;
     }
     if (wide) return launch_mx_wide(plan, L, q, p, st);
-    int cs = 1;
-    while (cs < kMxMaxCluster && 2 * cap * tiles * cs * 2 <= slots && kb / (cs * 2) >= 4) cs *= 2;
-    e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap, tiles), smem, st, wg, xm, p);
+    int cs = max(1, min(min(kMxMaxCluster, kb / 4), slots / (2 * cap * tiles)));
+    e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap, tiles), smem_of(stages), st, wg, xm, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_gateup_kernel");
-    p.w_scales = L->down_scales; p.x_scales = plan->mx_a_scales;
+    p.w_scales = L->down_scales; p.x_scales = plan->mx_a_scales; p.stages = down_stages;
     cs = max(1, min(min(kMxMaxCluster, cap), slots / (kb * tiles)));
-    e = launch_clusters(mx_down_kernel, dim3(cs, kb, tiles), smem, st, wd, am, p);
+    e = launch_clusters(mx_down_kernel, dim3(cs, kb, tiles), smem_of(down_stages), st, wd, am, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_down_kernel");
     plan->launches += 2;
     return CS_OK;
