@@ -121,6 +121,8 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
     if (mx) {
         alloc((void **)&p->mx_a, nt * cfg->d_ff);
         alloc((void **)&p->mx_a_scales, (nt + 127) / 128 * p->G * kMxTileBytes);
+        alloc((void **)&p->mx_done, ((nt + 255) / 256 + 1) * sizeof(unsigned));
+        if (e == cudaSuccess) e = cudaMemset(p->mx_done, 0, ((nt + 255) / 256 + 1) * sizeof(unsigned));
         alloc((void **)&p->mx_partial, mx_wide_partial_bytes(p));
     } else {
         alloc((void **)&p->x_host_in, nt * cfg->d * sizeof(float));
@@ -156,7 +158,7 @@ cs_status cs_plan_destroy(cs_plan *p) {
     cudaFree(p->resid_buf); cudaFree(p->fb_flags); cudaFree(p->fb_list); cudaFree(p->fb_count); cudaFree(p->colsum);
     cudaFree(p->status); cudaFree(p->x_host_in); cudaFree(p->x_host_out);
     cudaFree(p->mask); cudaFree(p->mask_count); cudaFree(p->counts); cudaFree(p->offsets); cudaFree(p->token_ids); cudaFree(p->glist);
-    cudaFree(p->mx_a); cudaFree(p->mx_a_scales); cudaFree(p->mx_partial);
+    cudaFree(p->mx_a); cudaFree(p->mx_a_scales); cudaFree(p->mx_partial); cudaFree(p->mx_done);
     cudaFree(p->nu); cudaFree(p->x_bf16); cudaFree(p->act); cudaFree(p->mma_partial);
     for (int i = 0; i < 2 * CS_STAGE_COUNT; ++i)
         if (p->ev[i] != nullptr) cudaEventDestroy(p->ev[i]);

@@ -26,6 +26,7 @@ constexpr int kMxThreads = 128 + 32 * kMxEpiWarps;   // weight loads, MMA, token
 constexpr int kMxMaxTile = 256;                      // tokens of a tile
 constexpr int kMxMaxStages = 8;
 constexpr int kMxMaxCluster = 8;
+constexpr int kMxReadyPolls = 16;
 constexpr int kMxPitch = 132;                        // floats from column to column of the spilled tile: float4 reads of 8 columns hit all banks
 constexpr int kMxNarrowTokens = 128;                 // larger batches take the pairs of mx_wide.cu
 
@@ -62,6 +63,8 @@ __device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t a, uint64_t b, ui
                  "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kMxEpiWarps) : "memory"); }
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
@@ -287,6 +290,8 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
                     const uint32_t at = (uint32_t)(c * kMxPitch + lane * 4) * 4;
                     *reinterpret_cast<float4 *>(smem + at) = sum_ranks(smem_u32(smem) + at, cs);
                 }
+            __syncwarp();
+            if (cs > 1) cluster_arrive();      // this warp is done with its peers' tiles
             epilogue_sync();
             // four threads to a column, sixteen channels each: a block of 32 is two neighbours'
             for (int i = threadIdx.x - 128;; i += 32 * kMxEpiWarps) {
@@ -319,7 +324,11 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
                 }
             }
         }
-        if (cs > 1) cluster_sync_all();      // peers are done with this CTA's tile
+        if (cs > 1) {      // until its peers are done with this CTA's
+            __syncwarp();
+            if (warp < 4) cluster_arrive();
+            cluster_wait();
+        }
     }
     mx_teardown(&bars, cols);
 }
@@ -332,8 +341,10 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int cs = gridDim.x, rank = blockIdx.x, z = blockIdx.z, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *smem = mx_setup(&bars, p.stages, cols, &wmap, &xmap);
     if (threadIdx.x == 0) {
-        unsigned ready;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(ready) : "l"(p.ready) : "memory");
+        // gate/up is running (this launch began on its trigger) and says so a microsecond in; a CTA that starts later sees it at once
+        unsigned ready = 0;
+        for (int poll = 0; poll < kMxReadyPolls && ready == 0; ++poll)
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(ready) : "l"(p.ready) : "memory");
         bars.all[0] = ready;
     }
     __syncthreads();
@@ -390,9 +401,8 @@ cudaError_t launch_clusters(void (*kernel)(const CUtensorMap, const CUtensorMap,
     return cudaLaunchKernelEx(&cfg, kernel, w, x, p);
 }
 
-constexpr int kMxBesideTokens = 32;
 constexpr int kMxSmemOne = 226 * 1024, kMxSmemTwo = 112 * 1024;   // a CTA's shared memory, alone on its SM or with another of its kind ...
-constexpr int kMxSmemGateUp = 126 * 1024, kMxSmemDown = 99 * 1024;   // ... or a gate/up CTA's beside a down CTA's
+constexpr int kMxSmemGateUp = 102 * 1024, kMxSmemDown = 61 * 1024;   // ... or a gate/up CTA's beside two down CTAs'
 
 }  // namespace
 
@@ -410,9 +420,9 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int rows = shared ? 1 : B;
     const bool wide = B > kMxNarrowTokens;
     const int tile = min(kMxMaxTile, (B + 15) / 16 * 16), tiles = (B + tile - 1) / tile;
-    // Shared memory.  Up to 32 tokens one CTA of each product fits on an SM beside the other, so that down's CTAs start, and load their weights, while
-    // gate/up runs; beyond, two CTAs of a product, or one where a tile has more than 128 tokens.
-    const bool beside = tile <= kMxBesideTokens, two = !beside && tile <= 128;
+    // Shared memory.  Where the weights are few (gate/up's tiles leave room for clusters of two on an SM each), one CTA of gate/up and two of down share an
+    // SM, so that down's CTAs start, and load their weights, while gate/up runs; otherwise two CTAs of a product, or one where a tile has more than 128 tokens.
+    const bool beside = tile <= 32 && 4 * cap <= plan->sm_count, two = !beside && tile <= 128;
     const int slots = plan->sm_count * (two ? 2 : 1);
     auto ring = [&](int bytes) { return max(2, min(kMxMaxStages, (bytes - 1024 - (int)sizeof(MxBars) - 64) / mx_stage_bytes(tile))); };
     const int stages = ring(beside ? kMxSmemGateUp : two ? kMxSmemTwo : kMxSmemOne), down_stages = beside ? ring(kMxSmemDown) : stages;
@@ -441,7 +451,7 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap, tiles), smem_of(stages), st, wg, xm, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_gateup_kernel");
     p.w_scales = L->down_scales; p.x_scales = plan->mx_a_scales; p.stages = down_stages;
-    cs = max(1, min(min(kMxMaxCluster, cap), slots / (kb * tiles)));
+    cs = max(1, min(min(kMxMaxCluster, cap), plan->sm_count * (beside ? 2 : 1) / (kb * tiles)));
     e = launch_clusters(mx_down_kernel, dim3(cs, kb, tiles), smem_of(down_stages), st, wd, am, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_down_kernel");
     plan->launches += 2;

@@ -30,11 +30,11 @@ static_assert(kWideStageBytes % 1024 == 0, "operands stand on 1024-byte boundari
 struct WideArgs {
     MxArgs p;
     int ztiles;        // token tiles
-    int width;         // output columns of a down item, 256 or 192
     int splits;        // parts of the list a down item is cut into; > 1: f32 results to `partial`
     int whole;         // the output's rows stand on 32-byte boundaries: whole sectors
     const uint8_t *down_codes, *down_scales;
-    float *partial;    // [item, split][256 tokens][256 columns]
+    float *partial;    // [down item and part][256 tokens][256 columns]
+    unsigned *done;    // [ztiles] epilogue warps that have stored their part of a token tile's activations; behind them the pairs that have ended
 };
 
 struct WideBars {
@@ -66,33 +66,55 @@ __device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 
-// What item `i` is.
+// Item i of a call: first every token tile's gate/up items, then the down items.  DB: 32-column blocks of a CTA's half of a down item.
 struct WideItem {
+    bool down;
     int z, col;            // token tile; list entry (gate/up) or first output column (down)
-    int first, n, part;    // its k blocks
+    int first, n;          // its k blocks
+    int index;             // of a down item and its part
 };
-template <bool DOWN> __device__ __forceinline__ int wide_items(const WideArgs &w, int count) {
-    return w.ztiles * (DOWN ? (w.p.d + w.width - 1) / w.width * w.splits : count);
-}
-template <bool DOWN> __device__ __forceinline__ WideItem wide_item(const WideArgs &w, int count, int i) {
+template <int DB> __host__ __device__ __forceinline__ int wide_across(int d) { return (d + 64 * DB - 1) / (64 * DB); }
+template <int DB> __device__ __forceinline__ WideItem wide_item(const WideArgs &w, int count, int i) {
     WideItem t;
-    const int across = DOWN ? (w.p.d + w.width - 1) / w.width : count;
-    t.part = DOWN ? i % w.splits : 0;
-    const int q = DOWN ? i / w.splits : i;
-    t.z = q / across;
-    t.col = (q - t.z * across) * (DOWN ? w.width : 1);
-    const int k = DOWN ? count : w.p.d >> 7, s = DOWN ? w.splits : 1;
-    t.first = k * t.part / s;
-    t.n = k * (t.part + 1) / s - t.first;
+    const int gate = w.ztiles * count;
+    t.down = i >= gate;
+    if (!t.down) {
+        t.z = i / count; t.col = i - t.z * count;
+        t.first = 0; t.n = w.p.d >> 7; t.index = 0;
+    } else {
+        t.index = i - gate;
+        const int across = wide_across<DB>(w.p.d), q = t.index / w.splits, part = t.index - q * w.splits;
+        t.z = q / across; t.col = (q - t.z * across) * (64 * DB);
+        t.first = count * part / w.splits; t.n = count * (part + 1) / w.splits - t.first;
+    }
     return t;
 }
 
-// BLOCKS: 32-column blocks of a CTA's half of the columns.
-template <bool DOWN, int BLOCKS> __global__ void __launch_bounds__(kWideThreads, 1)
-mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xs, const __grid_constant__ CUtensorMap tm_w,
-               const __grid_constant__ CUtensorMap tm_ws, const WideArgs w) {
+// Until all of a token tile's activations are in memory (bounded): they were stored by ordinary stores of other SMs and are read by TMA, so a proxy fence
+// stands on both sides.
+__device__ __forceinline__ bool wide_ready(const unsigned *done, unsigned need, uint32_t *aborted, DeviceStatus *status) {
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+        unsigned v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(done) : "memory");
+        if (v >= need) {
+            asm volatile("fence.proxy.async;" ::: "memory");
+            return true;
+        }
+        if (*reinterpret_cast<volatile uint32_t *>(aborted)) return false;
+        __nanosleep(100);
+    }
+    *reinterpret_cast<volatile uint32_t *>(aborted) = 1;
+    atomicCAS(&status->code, 0, (int)CS_ERR_TIMEOUT);
+    return false;
+}
+
+template <int DB> __global__ void __launch_bounds__(kWideThreads, 1)
+mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xs, const __grid_constant__ CUtensorMap tm_gu,
+               const __grid_constant__ CUtensorMap tm_gus, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_as,
+               const __grid_constant__ CUtensorMap tm_d, const __grid_constant__ CUtensorMap tm_ds, const WideArgs w) {
     extern __shared__ uint8_t raw[];
     __shared__ WideBars bars;
+    constexpr int kDownRows = 32 * DB;        // weight rows a CTA brings for a down item; 128 for gate/up
     const MxArgs &p = w.p;
     const uint32_t rank = cluster_ctarank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -103,7 +125,8 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         mbar_init(&bars.acc_empty, 2 * kWideEpiWarps);
         bars.aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (const CUtensorMap *m : {&tm_x, &tm_xs, &tm_w, &tm_ws}) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+        for (const CUtensorMap *m : {&tm_x, &tm_xs, &tm_gu, &tm_gus, &tm_a, &tm_as, &tm_d, &tm_ds})
+            asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     }
     if (warp == 1) {   // the same warp of both CTAs allocates for the pair
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512) : "memory");
@@ -126,25 +149,29 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
     }
     __syncthreads();
-    const int count = bars.count, items = wide_items<DOWN>(w, count);
-    constexpr int columns = 64 * BLOCKS, rows = columns >> 1;      // rows: the weight rows a CTA brings
-    if (!DOWN && p.fold && warp == 3) mx_check(p.support, p.entries, p.k, p.G, blockIdx.x, gridDim.x, p.status);
+    const int kb = p.d >> 7, count = bars.count, items = w.ztiles * (count + wide_across<DB>(p.d) * w.splits);
 
     if (warp == 0) {          // tokens, and the bytes both CTAs will bring
         if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
-            const uint32_t bytes = 2 * (128 * 128 + rows * 64 + 3 * kMxTileBytes);
             MxRing ring;
-            int fill = 0;
+            int fill = 0, ready = -1;
             for (int i = pair; i < items; i += pairs) {
-                const WideItem t = wide_item<DOWN>(w, count, i);
-                const int chunk = 2 * t.z + (int)rank;
+                const WideItem t = wide_item<DB>(w, count, i);
+                if (t.n == 0) continue;
+                if (t.down && t.z != ready) {
+                    if (!wide_ready(w.done + t.z, (unsigned)count * 2 * kWideEpiWarps, &bars.aborted, p.status)) goto done;
+                    ready = t.z;
+                }
+                const CUtensorMap *x = t.down ? &tm_a : &tm_x, *xs = t.down ? &tm_as : &tm_xs;
+                const uint32_t bytes = 2 * (128 * 128 + (t.down ? kDownRows : 128) * 64 + 3 * kMxTileBytes);
+                const int chunk = 2 * t.z + (int)rank, row = chunk * (t.down ? p.cap : kb);
                 for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
                     if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
                     uint8_t *st = smem + ring.stage * kWideStageBytes;
                     if (rank == 0) mbar_expect_tx(&bars.full[ring.stage], bytes);
-                    tma_load_2d_pair(st, &tm_x, j * 128, chunk * 128, full0 + 8u * ring.stage);
-                    tma_load_2d_pair(st + 128 * 128 + kMxWBytes, &tm_xs, 0, chunk * (DOWN ? p.cap : p.d >> 7) + j, full0 + 8u * ring.stage);
+                    tma_load_2d_pair(st, x, j * 128, chunk * 128, full0 + 8u * ring.stage);
+                    tma_load_2d_pair(st + 128 * 128 + kMxWBytes, xs, 0, row + j, full0 + 8u * ring.stage);
                     ring.next(kWideStages);
                 }
             }
@@ -155,21 +182,21 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             MxRing ring;
             int fill = 0, ahead = blockIdx.x;
             for (int i = pair; i < items; i += pairs) {
-                const WideItem t = wide_item<DOWN>(w, count, i);
-                const int kb = p.d >> 7;
-                // Gate/up: this CTA's half of the group.  Down: `rows` rows of W_down from where they stand, which may run into the next group's (columns
+                const WideItem t = wide_item<DB>(w, count, i);
+                const CUtensorMap *m = t.down ? &tm_d : &tm_gu, *ms = t.down ? &tm_ds : &tm_gus;
+                // Gate/up: this CTA's half of the group.  Down: rows of W_down from where they stand, which may run into the next group's (columns
                 // behind d, left out later); two tiles of scales from the one that holds the first column.
                 for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
                     if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
                     uint8_t *st = smem + ring.stage * kWideStageBytes + 128 * 128;
                     const uint32_t full = full0 + 8u * ring.stage;
-                    const int tile = DOWN ? bars.list[j] * kb + (t.col >> 7) : (bars.list[t.col] * kb + j) * 2;
-                    tma_load_2d_pair(st, &tm_w, 0, tile * 128 + (DOWN ? (t.col & 127) : 0) + (int)rank * rows, full);
-                    tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, &tm_ws, 0, tile, full);
-                    if (!DOWN && fill >= kWideStages && ahead < kb * count) {      // the down product's weights on their way to L2
-                        const size_t tile = (size_t)bars.list[ahead / kb] * kb + ahead % kb;
-                        prefetch_l2(w.down_codes + tile * kMxWLoad, kMxWLoad);
-                        prefetch_l2(w.down_scales + tile * kMxTileBytes, kMxTileBytes);
+                    const int tile = t.down ? bars.list[j] * kb + (t.col >> 7) : (bars.list[t.col] * kb + j) * 2;
+                    tma_load_2d_pair(st, m, 0, tile * 128 + (t.down ? (t.col & 127) + (int)rank * kDownRows : (int)rank * 128), full);
+                    tma_load_2d_pair(st + kMxWBytes + kMxTileBytes, ms, 0, tile, full);
+                    if (!t.down && fill >= kWideStages && ahead < kb * count) {      // the down product's weights on their way to L2
+                        const size_t next = (size_t)bars.list[ahead / kb] * kb + ahead % kb;
+                        prefetch_l2(w.down_codes + next * kMxWLoad, kMxWLoad);
+                        prefetch_l2(w.down_scales + next * kMxTileBytes, kMxTileBytes);
                         ahead += gridDim.x;
                     }
                     ring.next(kWideStages);
@@ -178,16 +205,16 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         }
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
-            uint32_t idesc[4];
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) idesc[kk] = wide_idesc(columns, kk);
             const uint32_t base = smem_u32(smem), tmem = bars.tmem;
             MxRing ring;
             int turn = 0;
             for (int i = pair; i < items; i += pairs) {
-                const WideItem t = wide_item<DOWN>(w, count, i);
+                const WideItem t = wide_item<DB>(w, count, i);
                 if (t.n == 0) continue;
-                const uint32_t shift = DOWN ? (uint32_t)(t.col & 127) >> 5 : 0;     // the first column's place in its tile of scales
+                uint32_t idesc[4];
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) idesc[kk] = wide_idesc(t.down ? 64 * DB : 256, kk);
+                const uint32_t shift = t.down ? (uint32_t)(t.col & 127) >> 5 : 0;     // the first column's place in its tile of scales
                 if (turn > 0 && !mx_wait(&bars.acc_empty, (turn - 1) & 1, &bars.aborted, p.status)) goto done;
                 tc_fence_after();
                 for (int j = 0; j < t.n; ++j) {
@@ -208,100 +235,113 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                 ++turn;
             }
         }
-    } else if (warp >= 4) {
+    } else if (warp == 3) {
+        if (p.fold) mx_check(p.support, p.entries, p.k, p.G, blockIdx.x, gridDim.x, p.status);
+    } else {
         const int quarter = warp & 3, half = (warp >> 2) - 1;      // lanes and half of the columns
         const uint32_t empty0 = map_to_cta(smem_u32(&bars.acc_empty), 0);
+        const uint32_t acc = bars.tmem + ((uint32_t)(quarter * 32) << 16);
         int turn = 0;
         for (int i = pair; i < items; i += pairs) {
-            __syncwarp();      // lanes without a token skip the end of an item
-            const WideItem t = wide_item<DOWN>(w, count, i);
+            __syncwarp();      // lanes without a token skip parts of an item
+            const WideItem t = wide_item<DB>(w, count, i);
             const int token = t.z * kWideTokens + (int)rank * 128 + quarter * 32 + lane;
-            bool member = true;      // whether this token uses the group; found while the products run
-            if (!DOWN && !p.shared && token < p.B) {
-                const int g = bars.list[t.col];
-                if (p.fold) {
-                    member = false;
-                    for (int j = 0; j < p.k; ++j) member |= ld_dep(p.support + (size_t)token * p.k + j) == g;
-                } else {
-                    member = ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1;
+            if (!t.down) {
+                bool member = p.shared;      // whether this token uses the group; found while the products run
+                if (!p.shared && token < p.B) {
+                    const int g = bars.list[t.col];
+                    if (p.fold)
+                        for (int j = 0; j < p.k; ++j) member |= ld_dep(p.support + (size_t)token * p.k + j) == g;
+                    else
+                        member = ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1;
                 }
-            }
-            __syncwarp();
-            uint32_t v[BLOCKS][32];
-            if (t.n > 0) {
+                __syncwarp();
                 if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
                 tc_fence_after();
-                const uint32_t at = bars.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * rows);
+                uint32_t v[4][32];
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) tc_ld32(at + 32 * b, v[b]);
+                for (int b = 0; b < 4; ++b) tc_ld32(acc + half * 128 + 32 * b, v[b]);
                 tc_wait_ld();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(empty0);
                 ++turn;
-            } else {
+                if (token < p.B) {
+                    uint32_t scales = 0;
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b)
+                    for (int b = 0; b < 2; ++b) {
+                        float m = 0.f;
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) v[b][c] = 0;
-            }
-            if (token >= p.B) continue;
-            if constexpr (!DOWN) {
-                uint32_t scales = 0;
+                        for (int c = 0; c < 32; ++c) {      // in place: the registers are what there is
+                            const float a = swiglu(__uint_as_float(v[b][c]), __uint_as_float(v[b + 2][c]));
+                            v[b][c] = __float_as_uint(a);
+                            m = max_abs(m, a);
+                        }
+                        const uint32_t byte = member ? mx_scale_byte<true>(__float_as_uint(m)) : 0u;
+                        const float inv = mx_inverse(byte);
+                        uint32_t o[8];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    float m = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {      // in place: the registers are what there is
-                        const float a = swiglu(__uint_as_float(v[b][c]), __uint_as_float(v[b + 2][c]));
-                        v[b][c] = __float_as_uint(a);
-                        m = max_abs(m, a);
+                        for (int c = 0; c < 8; ++c)
+                            o[c] = !member || byte == 255 ? 0u : pack_e4m3(__uint_as_float(v[b][4 * c]) * inv, __uint_as_float(v[b][4 * c + 1]) * inv,
+                                                                           __uint_as_float(v[b][4 * c + 2]) * inv, __uint_as_float(v[b][4 * c + 3]) * inv);
+                        store32(p.a + (size_t)token * p.cap * 128 + t.col * 128 + half * 64 + b * 32, o);
+                        scales |= byte << (8 * b);
                     }
-                    const uint32_t byte = member ? mx_scale_byte<true>(__float_as_uint(m)) : 0u;
-                    const float inv = mx_inverse(byte);
-                    uint32_t o[8];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        o[c] = !member || byte == 255 ? 0u : pack_e4m3(__uint_as_float(v[b][4 * c]) * inv, __uint_as_float(v[b][4 * c + 1]) * inv,
-                                                            __uint_as_float(v[b][4 * c + 2]) * inv, __uint_as_float(v[b][4 * c + 3]) * inv);
-                    store32(p.a + (size_t)token * p.cap * 128 + t.col * 128 + half * 64 + b * 32, o);
-                    scales |= byte << (8 * b);
+                    *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(token >> 7) * p.cap + t.col) * kMxTileBytes + (token & 31) * 16 +
+                                                  ((token & 127) >> 5) * 4 + half * 2) = (uint16_t)scales;
                 }
-                *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(token >> 7) * p.cap + t.col) * kMxTileBytes + (token & 31) * 16 +
-                                              ((token & 127) >> 5) * 4 + half * 2) = (uint16_t)scales;
+                asm volatile("fence.proxy.async;" ::: "memory");
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(w.done + t.z) : "memory");
             } else {
+                uint32_t v[DB][32];
+                if (t.n > 0) {
+                    if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
+                    tc_fence_after();
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    const int col = t.col + half * rows + 32 * b;
+                    for (int b = 0; b < DB; ++b) tc_ld32(acc + half * kDownRows + 32 * b, v[b]);
+                    tc_wait_ld();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(empty0);
+                    ++turn;
+                } else {
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[b][c] = 0;
+                }
+                if (token >= p.B) continue;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    const int col = t.col + half * kDownRows + 32 * b;
                     if (col >= p.d) break;
-                    if (w.splits == 1 && w.whole) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t o[8];
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) {
-                                const __nv_bfloat162 f = __floats2bfloat162_rn(__uint_as_float(v[b][16 * h + 2 * c]), __uint_as_float(v[b][16 * h + 2 * c + 1]));
-                                o[c] = *reinterpret_cast<const uint32_t *>(&f);
-                            }
-                            store32(p.out + (size_t)token * p.d + col + 16 * h, o);
-                        }
-                    } else if (w.splits == 1) {
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            __nv_bfloat162 f[4];
-#pragma unroll
-                            for (int c = 0; c < 4; ++c)
-                                f[c] = __floats2bfloat162_rn(__uint_as_float(v[b][8 * h + 2 * c]), __uint_as_float(v[b][8 * h + 2 * c + 1]));
-                            *reinterpret_cast<uint4 *>(p.out + (size_t)token * p.d + col + 8 * h) = *reinterpret_cast<const uint4 *>(f);
-                        }
-                    } else {
-                        float *to = w.partial + ((size_t)i * kWideTokens + token - t.z * kWideTokens) * 256 + half * rows + 32 * b;
+                    if (w.splits > 1) {
+                        float *to = w.partial + ((size_t)t.index * kWideTokens + token - t.z * kWideTokens) * 256 + half * kDownRows + 32 * b;
 #pragma unroll
                         for (int h = 0; h < 4; ++h) {
                             uint32_t o[8];
 #pragma unroll
                             for (int c = 0; c < 8; ++c) o[c] = v[b][8 * h + c];
                             store32(to + 8 * h, o);
+                        }
+                        continue;
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t o[8];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const __nv_bfloat162 f = __floats2bfloat162_rn(__uint_as_float(v[b][16 * h + 2 * c]), __uint_as_float(v[b][16 * h + 2 * c + 1]));
+                            o[c] = *reinterpret_cast<const uint32_t *>(&f);
+                        }
+                        __nv_bfloat16 *to = p.out + (size_t)token * p.d + col + 16 * h;
+                        if (w.whole) {
+                            store32(to, o);
+                        } else {
+                            reinterpret_cast<uint4 *>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                            reinterpret_cast<uint4 *>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
                         }
                     }
                 }
@@ -319,18 +359,24 @@ done:
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(bars.tmem), "r"(512) : "memory");
     }
+    // the last pair to end clears the counters for the next call
+    if (threadIdx.x == 0 && rank == 0) {
+        __threadfence();
+        if (atomicAdd(w.done + w.ztiles, 1u) == (unsigned)pairs - 1)
+            for (int z = 0; z <= w.ztiles; ++z) w.done[z] = 0;
+    }
 }
 
 // out[t, c] = the sum of an item's parts, in their order.  Four columns a thread.
 __global__ void __launch_bounds__(256)
-mx_wide_sum_kernel(const WideArgs w) {
+mx_wide_sum_kernel(const WideArgs w, int width) {
     pdl_launch_dependents();
     pdl_wait();
-    const int across = (w.p.d + w.width - 1) / w.width, d4 = w.p.d >> 2;
+    const int across = (w.p.d + width - 1) / width, d4 = w.p.d >> 2;
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= w.p.B * d4) return;
-    const int t = i / d4, c = (i - t * d4) * 4, z = t / kWideTokens, x = c / w.width;
-    const float *from = w.partial + ((size_t)(z * across + x) * w.splits * kWideTokens + t - z * kWideTokens) * 256 + c - x * w.width;
+    const int t = i / d4, c = (i - t * d4) * 4, z = t / kWideTokens, x = c / width;
+    const float *from = w.partial + ((size_t)(z * across + x) * w.splits * kWideTokens + t - z * kWideTokens) * 256 + c - x * width;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s = 0; s < w.splits; ++s) {
         const float4 u = ld_dep4(from + (size_t)s * kWideTokens * 256);
@@ -352,24 +398,11 @@ bool make_map_scales(CUtensorMap *map, const void *base, uint64_t tiles, uint32_
 
 constexpr size_t kWideSmem = 1024 + (size_t)kWideStages * kWideStageBytes;
 
-template <bool DOWN, int BLOCKS>
-cudaError_t launch_wide(int pairs, cudaStream_t st, const CUtensorMap &x, const CUtensorMap &xs, const CUtensorMap &wt, const CUtensorMap &ws, const WideArgs &w) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = kWideSmem; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, mx_wide_kernel<DOWN, BLOCKS>, x, xs, wt, ws, w);
-}
-
 }  // namespace
 
 cs_status prepare_mx_wide(cs_plan *plan) {
     (void)plan;
-    for (auto *k : {mx_wide_kernel<false, 4>, mx_wide_kernel<true, 4>, mx_wide_kernel<true, 3>})
+    for (auto *k : {mx_wide_kernel<3>, mx_wide_kernel<4>})
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kWideSmem) != cudaSuccess || prefer_shared(k) != cudaSuccess)
             return CS_ERR_CUDA;
     return prefer_shared(mx_wide_sum_kernel) == cudaSuccess ? CS_OK : CS_ERR_CUDA;
@@ -378,36 +411,42 @@ cs_status prepare_mx_wide(cs_plan *plan) {
 size_t mx_wide_partial_bytes(const cs_plan *plan) { return (size_t)(plan->sm_count / 2) * kWideTokens * 256 * sizeof(float); }
 
 cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const MxArgs &args, cudaStream_t st) {
-    const int kb = args.d / 128, G = args.G, B = args.B, chunks = (B + 127) / 128, pairs = plan->sm_count / 2;
+    const int d = args.d, kb = d / 128, G = args.G, B = args.B, chunks = (B + 127) / 128, pairs = plan->sm_count / 2;
     WideArgs w;
     w.p = args;
     w.ztiles = (B + kWideTokens - 1) / kWideTokens;
-    w.partial = plan->mx_partial;
+    w.partial = plan->mx_partial; w.done = plan->mx_done;
     w.down_codes = L->down_codes; w.down_scales = L->down_scales;
-    w.splits = 1;
     w.whole = reinterpret_cast<uintptr_t>(args.out) % 32 == 0;
     // Output columns of a down item: the width whose rounds over the pairs cost least (13B shape, 2048 tokens: 160 items of 256 are three rounds, 216
     // of 192 three rounds of 3/4).
-    auto cost = [&](int width) { return (((args.d + width - 1) / width * w.ztiles + pairs - 1) / pairs) * width; };
-    w.width = cost(192) < cost(256) ? 192 : 256;
-    const int items = (args.d + w.width - 1) / w.width * w.ztiles;
-    // Fewer items than pairs: cut the list, into parts of at least four k blocks
-    if (2 * items <= pairs) w.splits = max(1, min(min(pairs / items, 8), args.cap / 4));
+    const int n256 = wide_across<4>(d) * w.ztiles, n192 = wide_across<3>(d) * w.ztiles;
+    const bool narrow = (n192 + pairs - 1) / pairs * 3 < (n256 + pairs - 1) / pairs * 4;
+    const int width = narrow ? 192 : 256, items = narrow ? n192 : n256;
+    // Fewer items than half the pairs: cut the list, into parts of at least four k blocks
+    w.splits = 2 * items <= pairs ? max(1, min(min(pairs / items, 8), args.cap / 4)) : 1;
     CUtensorMap x, xs, wg, wgs, a, as, wd, wds;
-    if (!make_map_bytes(&x, q, args.d, B, 128) || !make_map_scales(&xs, args.x_scales, (uint64_t)chunks * kb, 1) ||
-        !make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb, 128) || !make_map_scales(&wgs, L->gate_up_scales, (uint64_t)2 * G * kb, 2) ||
+    if (!make_map_bytes(&x, q, d, B, 128) || !make_map_scales(&xs, args.x_scales, (uint64_t)chunks * kb, 1) ||
+        !make_map_tiles(&wg, L->gate_up_codes, (uint64_t)2 * G * kb) || !make_map_scales(&wgs, L->gate_up_scales, (uint64_t)2 * G * kb, 2) ||
         !make_map_bytes(&a, plan->mx_a, (uint64_t)args.cap * 128, B, 128) || !make_map_scales(&as, plan->mx_a_scales, (uint64_t)chunks * args.cap, 1) ||
-        !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G, w.width / 2) || !make_map_scales(&wds, L->down_scales, (uint64_t)kb * G, 2)) {
+        !make_map_tiles(&wd, L->down_codes, (uint64_t)kb * G, width / 2) || !make_map_scales(&wds, L->down_scales, (uint64_t)kb * G, 2)) {
         snprintf(plan->cuda_error, sizeof plan->cuda_error, "cuTensorMapEncodeTiled failed");
         return CS_ERR_CUDA;
     }
-    cudaError_t e = launch_wide<false, 4>(pairs, st, x, xs, wg, wgs, w);
-    if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<gate/up>");
-    e = (w.width == 256 ? launch_wide<true, 4> : launch_wide<true, 3>)(min(pairs, items * w.splits), st, a, as, wd, wds, w);
-    if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel<down>");
-    plan->launches += 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (unsigned)min((int64_t)pairs, (int64_t)w.ztiles * args.cap + (int64_t)items * w.splits));
+    cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = kWideSmem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, narrow ? mx_wide_kernel<3> : mx_wide_kernel<4>, x, xs, wg, wgs, a, as, wd, wds, w);
+    if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_kernel");
+    plan->launches += 1;
     if (w.splits > 1) {
-        e = launch_pdl(true, mx_wide_sum_kernel, dim3((B * (args.d / 4) + 255) / 256), dim3(256), 0, st, w);
+        e = launch_pdl(true, mx_wide_sum_kernel, dim3((unsigned)(((int64_t)B * (d / 4) + 255) / 256)), dim3(256), 0, st, w, width);
         if (e != cudaSuccess) return record_cuda(plan, e, "mx_wide_sum_kernel");
         plan->launches += 1;
     }
