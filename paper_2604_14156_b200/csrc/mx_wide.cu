@@ -90,8 +90,8 @@ template <int DB> __device__ __forceinline__ WideItem wide_item(const WideArgs &
     return t;
 }
 
-// Until all of a token tile's activations are in memory (bounded): they were stored by ordinary stores of other SMs and are read by TMA, so a proxy fence
-// stands on both sides.
+// Until all of a token tile's activations are in memory (bounded).  They were stored by ordinary stores of other SMs and are read by TMA, so a proxy fence
+// stands between the acquire and the loads.
 __device__ __forceinline__ bool wide_ready(const unsigned *done, unsigned need, uint32_t *aborted, DeviceStatus *status) {
     for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
         unsigned v;
@@ -290,9 +290,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                     *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(token >> 7) * p.cap + t.col) * kMxTileBytes + (token & 31) * 16 +
                                                   ((token & 127) >> 5) * 4 + half * 2) = (uint16_t)scales;
                 }
-                asm volatile("fence.proxy.async;" ::: "memory");
-                __threadfence();
-                __syncwarp();
+                __syncwarp();      // one lane's release covers the warp's stores; a fence in each lane cost 3 us an item
                 if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(w.done + t.z) : "memory");
             } else {
                 uint32_t v[DB][32];
