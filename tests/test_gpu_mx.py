@@ -375,6 +375,32 @@ def test_ffn_captured_replayed_and_on_two_streams():
         x.plan.close()
 
 
+@pytest.mark.parametrize("B,d,G,k", [(1, 4096, 40, 22), (3, 4096, 40, 22), (16, 2048, 16, 7), (40, 4096, 40, 12), (64, 4096, 40, 22), (100, 2048, 16, 7), (128, 1024, 16, 7),
+                                     (200, 2048, 40, 12), (300, 1024, 16, 7)])
+def test_ffn_many_calls_back_to_back(B, d, G, k):
+    """Launches that overlap their predecessors' ends, thousands of times: every result is the first one."""
+    ps = [Problem(B, d, G, k, False, seed=s) for s in (4, 5)]
+    want = [p.run() for p in ps]
+    outs = [torch.zeros_like(w) for w in want]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(10):
+            for p, o in zip(ps, outs):
+                p.run(out=o)
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for _ in range(100):
+        for o in outs:
+            o.fill_(7)
+        graph.replay()
+        for o, w in zip(outs, want):
+            wrong += (o != w).sum()
+    assert int(wrong) == 0
+    for p, o in zip(ps, outs):
+        p.check(o)
+        p.plan.close()
+
+
 def test_ffn_refusals():
     p = Problem(8, 256, 4, 2, False)
     with pytest.raises(ValueError):
