@@ -332,7 +332,7 @@ cs_status cs_ffn_exec_shared(cs_plan *plan, const cs_layer *layer, const void *H
  * Microscaled low precision: weights in four bits, activations in eight, in blocks of 32 consecutive elements that share a
  * power of two (the OCP layouts mxfp4 and mxfp8).  A plan for it has w_dtype = CS_MX4, group = 128 and d a multiple of 128
  * (CS_ERR_UNSUPPORTED otherwise); its sensor and estimator calls are those of any plan, its actuator is cs_mx_ffn /
- * cs_mx_ffn_shared, and the calls that take a cs_layer return CS_ERR_UNSUPPORTED.  One layer of a decode step:
+ * cs_mx_ffn_shared, and the calls that take a cs_layer return CS_ERR_UNSUPPORTED; stage timing does not cover the cs_mx_ calls.  One layer of a decode step:
  *     cs_mx_norm (residual, n, q, s) -> cs_sketch(n) -> cs_recover -> cs_mx_ffn(q, s) -> the next cs_mx_norm's delta.
  *
  * A block whose largest magnitude is amax has the scale 2^e, e the smallest integer >= -127 with amax <= M 2^e, where M is
@@ -382,7 +382,7 @@ cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_
  *   -> x_out [B,d] of x's type (may be x or NULL), n_out [B,d] f32 or NULL (what cs_sketch reads), q [B,d] e4m3 bytes,
  *   s [ceil(B/128), d/128, 512] bytes: the scale of row r, block b at byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of tile
  *   (r / 128, b / 4), the order in which block-scaled tensor-core products read scales; scales of rows from B on are 0.
- * A NaN makes its row NaN, an infinity its block (the rest of such a row is 0); rows keep to themselves.  Other than x_out = x (and delta = n_out or x_out), outputs overlap no input.
+ * A NaN makes its row NaN, an infinity its block (the rest of such a row is 0); rows keep to themselves.  Other than x_out = x, outputs overlap no input.
  * Pointers are 16-byte aligned.  No scratch of the plan is used.
  */
 cs_status cs_mx_norm(cs_plan *plan, const void *x, int32_t x_dtype, const void *delta, int32_t delta_dtype, const float *gamma,

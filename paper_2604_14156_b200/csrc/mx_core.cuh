@@ -21,7 +21,6 @@ struct MxArgs {
     int tile, stages;               // tokens of a tile, ring stages
     int entries;                    // of the support
     int shared, fold;               // one support for all tokens; gate/up makes the list
-    int w_once;                     // weights are read by one token tile only
 };
 
 // A batch on CTA pairs (mx_wide.cu); the list stands in p.list unless p.fold.

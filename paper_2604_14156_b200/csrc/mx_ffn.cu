@@ -23,12 +23,11 @@ namespace {
 
 constexpr int kMxEpiWarps = 8;
 constexpr int kMxThreads = 128 + 32 * kMxEpiWarps;   // weight loads, MMA, token loads, one idle warp; epilogue
-constexpr int kMxMaxTile = 256;                      // tokens of a tile
 constexpr int kMxMaxStages = 8;
 constexpr int kMxMaxCluster = 8;
 constexpr int kMxReadyPolls = 16;
 constexpr int kMxPitch = 132;                        // floats from column to column of the spilled tile: float4 reads of 8 columns hit all banks
-constexpr int kMxNarrowTokens = 128;                 // larger batches take the pairs of mx_wide.cu
+constexpr int kMxNarrowTokens = 128, kMxNarrowShared = 192, kMxMaxTile = 192;   // larger batches take the pairs of mx_wide.cu, see launch_mx_ffn
 
 struct MxBars {
     uint64_t full[kMxMaxStages], empty[kMxMaxStages], acc;
@@ -118,7 +117,7 @@ mx_list_kernel(const int32_t *support, int rows, int k, int G, uint32_t *mask, i
 
 struct MxRange { int first, n; };
 
-// Three warps feed and run the products of k blocks [r.first, r.first + r.n) against token tile z.  Weight tile of k block j: wtile + 2 j, or with DOWN
+// Three warps feed and run the products of k blocks [r.first, r.first + r.n) against the batch.  Weight tile of k block j: wtile + 2 j, or with DOWN
 // wtile + (d / 128) list[j].
 template <bool DOWN>
 __device__ __forceinline__ void mx_load_weights(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, int wtile, MxRange r) {
@@ -131,17 +130,14 @@ __device__ __forceinline__ void mx_load_weights(const CUtensorMap *map, const Mx
         uint64_t *full = &bars->full[ring.stage];
         const int tile = DOWN ? wtile + bars->list[r.first + i] * (p.d >> 7) : wtile + 2 * (r.first + i);
         mbar_expect_tx(full, kMxWLoad + kMxTileBytes);
-        if (p.w_once) tma_load_2d(w, map, 0, tile * 128, full, policy);
-        else tma_load_2d(w, map, 0, tile * 128, full);
+        tma_load_2d(w, map, 0, tile * 128, full, policy);
         bulk_load(w + scales, p.w_scales + (size_t)tile * kMxTileBytes, kMxTileBytes, full);
         ring.next(p.stages);
     }
 }
-__device__ __forceinline__ void mx_load_tokens(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int z, int kpitch) {
+__device__ __forceinline__ void mx_load_tokens(const CUtensorMap *map, const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int kpitch) {
     const int stage_bytes = mx_stage_bytes(p.tile), chunks = mx_chunks(p.tile);
-    // behind the last row: any tile of scales that exists
-    const uint8_t *s0 = p.x_scales + (size_t)min(z * p.tile >> 7, (p.B - 1) >> 7) * kpitch * kMxTileBytes;
-    const uint8_t *s1 = p.x_scales + (size_t)min((z * p.tile >> 7) + 1, (p.B - 1) >> 7) * kpitch * kMxTileBytes;
+    const uint8_t *s0 = p.x_scales, *s1 = s0 + (p.B > 128 ? (size_t)kpitch * kMxTileBytes : 0);      // a tile of 144 has a second tile of scales
     MxRing ring;
     for (int i = 0; i < r.n; ++i) {
         if (i >= p.stages && !mx_wait(&bars->empty[ring.stage], ring.phase ^ 1, &bars->aborted, p.status)) return;
@@ -149,18 +145,18 @@ __device__ __forceinline__ void mx_load_tokens(const CUtensorMap *map, const MxA
         uint64_t *full = &bars->full[ring.stage];
         const int j = r.first + i;
         mbar_expect_tx(full, p.tile * 128 + kMxTileBytes * chunks);
-        tma_load_2d(x, map, j * 128, z * p.tile, full);
+        tma_load_2d(x, map, j * 128, 0, full);
         uint8_t *sc = x + p.tile * 128 + kMxTileBytes;
         bulk_load(sc, s0 + (size_t)j * kMxTileBytes, kMxTileBytes, full);
         if (chunks > 1) bulk_load(sc + kMxTileBytes, s1 + (size_t)j * kMxTileBytes, kMxTileBytes, full);
         ring.next(p.stages);
     }
 }
-__device__ __forceinline__ void mx_products(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int columns) {
+__device__ __forceinline__ void mx_products(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r) {
     const int stage_bytes = mx_stage_bytes(p.tile), chunks = mx_chunks(p.tile);
     uint32_t idesc[4];
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) idesc[kk] = mx_idesc(columns, kk);
+    for (int kk = 0; kk < 4; ++kk) idesc[kk] = mx_idesc(p.tile, kk);
     const uint32_t base = smem_u32(smem), tmem = bars->tmem;
     MxRing ring;
     for (int i = 0; i < r.n; ++i) {
@@ -180,17 +176,17 @@ __device__ __forceinline__ void mx_products(const MxArgs &p, uint8_t *smem, MxBa
     if (r.n > 0) tc_commit(&bars->acc);
 }
 // The accumulators of the tile's valid tokens to shared memory, [column][kMxPitch], over the drained ring; zeros where there was no k block.
-__device__ __forceinline__ void mx_spill(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r, int valid) {
+__device__ __forceinline__ void mx_spill(const MxArgs &p, uint8_t *smem, MxBars *bars, MxRange r) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
     float *tile = reinterpret_cast<float *>(smem) + quarter * 32 + lane;
     const bool ok = r.n > 0 && mx_wait(&bars->acc, 0, &bars->aborted, p.status);
     tc_fence_after();
-    for (int c = 16 * ((warp >> 2) - 1); c < valid; c += 32) {
+    for (int c = 16 * ((warp >> 2) - 1); c < p.B; c += 32) {
         uint32_t v[16];
         if (ok) { tc_ld16(bars->tmem + ((uint32_t)quarter << 21) + c, v); tc_wait_ld(); }
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (c + j < valid) tile[(c + j) * kMxPitch] = ok ? __uint_as_float(v[j]) : 0.f;
+            if (c + j < p.B) tile[(c + j) * kMxPitch] = ok ? __uint_as_float(v[j]) : 0.f;
     }
 }
 
@@ -235,16 +231,16 @@ __device__ __forceinline__ void mx_teardown(MxBars *bars, int cols) {
     }
 }
 
-// Grid (cluster, 2 cap, token tiles): tile y is one half (64 channels) of list entry y / 2; the CTAs of a cluster split d.
+// Grid (cluster, 2 cap): tile y is one half (64 channels) of list entry y / 2; the CTAs of a cluster split d.
 __global__ void __launch_bounds__(kMxThreads)
 mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const MxArgs p) {
     __shared__ MxBars bars;
-    const int cs = gridDim.x, rank = blockIdx.x, entry = blockIdx.y >> 1, half = blockIdx.y & 1, z = blockIdx.z;
+    const int cs = gridDim.x, rank = blockIdx.x, entry = blockIdx.y >> 1, half = blockIdx.y & 1;
     const int kb = p.d >> 7, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *smem = mx_setup(&bars, p.stages, cols, &wmap, &xmap);
     pdl_wait();
     pdl_launch_dependents();
-    const bool first = blockIdx.x + blockIdx.y + blockIdx.z == 0;
+    const bool first = blockIdx.x + blockIdx.y == 0;
     if (p.fold) {
         if (threadIdx.x < 4 + kMxMaxTile / 32) (threadIdx.x < 4 ? bars.all[threadIdx.x] : bars.bits[threadIdx.x - 4]) = 0;
         __syncthreads();
@@ -265,28 +261,27 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
         }
         if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(p.ready) : "memory");
     }
-    if (p.fold && warp == 3 && blockIdx.x + blockIdx.z == 0) mx_check(p.support, p.entries, p.k, p.G, blockIdx.y, gridDim.y, p.status);
+    if (p.fold && warp == 3 && blockIdx.x == 0) mx_check(p.support, p.entries, p.k, p.G, blockIdx.y, gridDim.y, p.status);
     if (entry < bars.count) {      // the same in every CTA of a cluster
         const int g = bars.list[entry];
-        const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
         const MxRange r = {kb * rank / cs, kb * (rank + 1) / cs - kb * rank / cs};
         if (warp == 0) {
             if (elect_one()) mx_load_weights<false>(&wmap, p, smem, &bars, 2 * g * kb + half, r);
         } else if (warp == 1) {
-            if (elect_one()) mx_products(p, smem, &bars, r, columns);
+            if (elect_one()) mx_products(p, smem, &bars, r);
         } else if (warp == 2) {
-            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, z, kb);
+            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, kb);
         } else if (warp >= 4) {
             if (p.fold && !p.shared)      // while the products run: who uses this group
-                for (int t = threadIdx.x - 128; t < valid * p.k; t += 32 * kMxEpiWarps)
-                    if (ld_dep(p.support + (size_t)z * p.tile * p.k + t) == g) atomicOr(&bars.bits[t / p.k >> 5], 1u << (t / p.k & 31));
-            mx_spill(p, smem, &bars, r, valid);
+                for (int t = threadIdx.x - 128; t < p.entries; t += 32 * kMxEpiWarps)
+                    if (ld_dep(p.support + t) == g) atomicOr(&bars.bits[t / p.k >> 5], 1u << (t / p.k & 31));
+            mx_spill(p, smem, &bars, r);
         }
         __syncwarp();
         if (cs > 1) cluster_sync_all();
         if (warp >= 4) {
             if (cs > 1)      // this CTA's columns, every cs-th, summed in place: no other CTA reads them
-                for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
+                for (int c = (warp - 4) * cs + rank; c < p.B; c += kMxEpiWarps * cs) {
                     const uint32_t at = (uint32_t)(c * kMxPitch + lane * 4) * 4;
                     *reinterpret_cast<float4 *>(smem + at) = sum_ranks(smem_u32(smem) + at, cs);
                 }
@@ -295,10 +290,10 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
             epilogue_sync();
             // four threads to a column, sixteen channels each: a block of 32 is two neighbours'
             for (int i = threadIdx.x - 128;; i += 32 * kMxEpiWarps) {
-                const int c = (i >> 2) * cs + rank, part = i & 3, t = z * p.tile + c;
-                if (__all_sync(0xffffffffu, c >= valid)) break;
-                const bool in = c < valid;
-                const bool member = in && (p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * (size_t)t + (g >> 5)] >> (g & 31) & 1));
+                const int c = (i >> 2) * cs + rank, part = i & 3;
+                if (__all_sync(0xffffffffu, c >= p.B)) break;
+                const bool in = c < p.B;
+                const bool member = in && (p.shared || (p.fold ? bars.bits[c >> 5] >> (c & 31) & 1 : p.mask[4 * c + (g >> 5)] >> (g & 31) & 1));
                 const float4 *gate = reinterpret_cast<const float4 *>(smem) + (in ? c * (kMxPitch / 4) : 0) + part * 4, *up = gate + 16;
                 float a[16], m = 0.f;
 #pragma unroll
@@ -317,9 +312,9 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
                     o[j] = !member || byte == 255 ? 0u : pack_e4m3(a[4 * j] * inv, a[4 * j + 1] * inv, a[4 * j + 2] * inv, a[4 * j + 3] * inv);
                 const uint32_t other = __shfl_down_sync(0xffffffffu, byte, 2);
                 if (in) {
-                    *reinterpret_cast<uint4 *>(p.a + (size_t)t * p.cap * 128 + entry * 128 + half * 64 + part * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4 *>(p.a + (size_t)c * p.cap * 128 + entry * 128 + half * 64 + part * 16) = make_uint4(o[0], o[1], o[2], o[3]);
                     if (part == 0)
-                        *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(t >> 7) * p.cap + entry) * kMxTileBytes + (t & 31) * 16 + ((t & 127) >> 5) * 4 + half * 2) =
+                        *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(c >> 7) * p.cap + entry) * kMxTileBytes + (c & 31) * 16 + ((c & 127) >> 5) * 4 + half * 2) =
                             (uint16_t)(byte | other << 8);
                 }
             }
@@ -333,12 +328,12 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
     mx_teardown(&bars, cols);
 }
 
-// Grid (cluster, d / 128, token tiles): the CTAs of a cluster split the list.  Weights depend on the list alone: where gate/up, which is still
+// Grid (cluster, d / 128): the CTAs of a cluster split the list.  Weights depend on the list alone: where gate/up, which is still
 // running, has said that it stands, their loads start before the wait for gate/up's result.
 __global__ void __launch_bounds__(kMxThreads)
 mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const MxArgs p) {
     __shared__ MxBars bars;
-    const int cs = gridDim.x, rank = blockIdx.x, z = blockIdx.z, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cs = gridDim.x, rank = blockIdx.x, cols = mx_tmem_cols(p.tile, p.stages), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *smem = mx_setup(&bars, p.stages, cols, &wmap, &xmap);
     if (threadIdx.x == 0) {
         // gate/up is running (this launch began on its trigger) and says so a microsecond in; a CTA that starts later sees it at once
@@ -353,7 +348,6 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
     __syncthreads();
     const int n = bars.count;
-    const int valid = min(p.tile, p.B - z * p.tile), columns = (valid + 15) & ~15;
     const MxRange r = {n * rank / cs, n * (rank + 1) / cs - n * rank / cs};
     if (warp == 0) {
         if (elect_one()) mx_load_weights<true>(&wmap, p, smem, &bars, blockIdx.y, r);
@@ -362,13 +356,13 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     } else {
         pdl_wait();
         pdl_launch_dependents();
-        if (warp == 3 && lane == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) *p.ready = 0;
+        if (warp == 3 && lane == 0 && blockIdx.x + blockIdx.y == 0) *p.ready = 0;
         if (warp == 1) {
-            if (elect_one()) mx_products(p, smem, &bars, r, columns);
+            if (elect_one()) mx_products(p, smem, &bars, r);
         } else if (warp == 2) {
-            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, z, p.cap);
+            if (elect_one()) mx_load_tokens(&xmap, p, smem, &bars, r, p.cap);
         } else if (warp >= 4) {
-            mx_spill(p, smem, &bars, r, valid);
+            mx_spill(p, smem, &bars, r);
         }
         __syncwarp();
     }
@@ -376,11 +370,11 @@ mx_down_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     if (warp >= 4) {
         if (cs == 1) epilogue_sync();
 #pragma unroll 2
-        for (int c = (warp - 4) * cs + rank; c < valid; c += kMxEpiWarps * cs) {
+        for (int c = (warp - 4) * cs + rank; c < p.B; c += kMxEpiWarps * cs) {
             const uint32_t at = (uint32_t)(c * kMxPitch + lane * 4) * 4;
             const float4 v = cs == 1 ? *reinterpret_cast<const float4 *>(smem + at) : sum_ranks(smem_u32(smem) + at, cs);
             const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-            *reinterpret_cast<uint2 *>(p.out + (size_t)(z * p.tile + c) * p.d + blockIdx.y * 128 + lane * 4) =
+            *reinterpret_cast<uint2 *>(p.out + (size_t)c * p.d + blockIdx.y * 128 + lane * 4) =
                 make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
         }
     }
@@ -418,8 +412,12 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int d = plan->cfg.d, k = plan->cfg.k, G = plan->G, kb = d / 128;
     const int cap = shared ? k : (int)min((int64_t)G, (int64_t)B * k);
     const int rows = shared ? 1 : B;
-    const bool wide = B > kMxNarrowTokens;
-    const int tile = min(kMxMaxTile, (B + 15) / 16 * 16), tiles = (B + tile - 1) / tile;
+    // Which kernels.  Pairs take 256 tokens for the price of one, but a group to an item: few groups leave most pairs without one.  Narrow against wide, us:
+    // own supports, 22 of 86 groups of d = 4096, 128 tokens 40.8 and 47.0, 129 (one CTA to an SM) 50.7 and 47.0, 200 56.5 and 48.4; 6 of 24 of 1024, 128 tokens
+    // 17.4 and 20.3, 129 21.4 and 20.5; 12 of 48 of 2048, where the line is late, 64 tokens 25.0 and 23.8, 128 32.8 and 25.9.  Shared, 22 groups of
+    // 4096, 129 tokens 24.1 and 28.9, 200 28.1 and 29.3, 256 31.1 and 30.2; 54 of 5120, 160 tokens 34.7 and 36.6, 200 37.5 and 37.1.
+    const bool wide = B > (shared && 2 * cap <= plan->sm_count ? kMxNarrowShared : kMxNarrowTokens);
+    const int tile = min(kMxMaxTile, (B + 15) / 16 * 16);
     // Shared memory.  Where the weights are few (gate/up's tiles leave room for clusters of two on an SM each), one CTA of gate/up and two of down share an
     // SM, so that down's CTAs start, and load their weights, while gate/up runs; otherwise two CTAs of a product, or one where a tile has more than 128 tokens.
     const bool beside = tile <= 32 && 4 * cap <= plan->sm_count, two = !beside && tile <= 128;
@@ -437,7 +435,7 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     p.support = support; p.list = plan->glist; p.count = plan->nu; p.ready = plan->mask_count; p.mask = plan->mask;
     p.w_scales = L->gate_up_scales; p.x_scales = s;
     p.a = plan->mx_a; p.a_scales = plan->mx_a_scales; p.out = static_cast<__nv_bfloat16 *>(out); p.status = plan->status;
-    p.B = B; p.d = d; p.G = G; p.k = k; p.cap = cap; p.tile = tile; p.stages = stages; p.shared = shared; p.w_once = tiles == 1;
+    p.B = B; p.d = d; p.G = G; p.k = k; p.cap = cap; p.tile = tile; p.stages = stages; p.shared = shared;
     p.entries = (int)min((int64_t)rows * k, (int64_t)1 << 30);
     p.fold = p.entries <= (wide ? kWideFoldEntries : kMxFoldEntries);
     cudaError_t e;
@@ -447,13 +445,16 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
         plan->launches += 1;
     }
     if (wide) return launch_mx_wide(plan, L, q, p, st);
-    int cs = max(1, min(min(kMxMaxCluster, kb / 4), slots / (2 * cap * tiles)));
-    e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap, tiles), smem_of(stages), st, wg, xm, p);
+    int cs = max(1, min(min(kMxMaxCluster, kb / 4), slots / (2 * cap)));
+    e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap), smem_of(stages), st, wg, xm, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_gateup_kernel");
     p.w_scales = L->down_scales; p.x_scales = plan->mx_a_scales; p.stages = down_stages;
-    cs = max(1, min(min(kMxMaxCluster, cap), plan->sm_count * (beside ? 2 : 1) / (kb * tiles)));
-    e = launch_clusters(mx_down_kernel, dim3(cs, kb, tiles), smem_of(down_stages), st, wd, am, p);
-    if (e != cudaSuccess) return record_cuda(plan, e, "mx_down_kernel");
+    cs = max(1, min(min(kMxMaxCluster, cap), plan->sm_count * (beside ? 2 : 1) / kb));
+    e = launch_clusters(mx_down_kernel, dim3(cs, kb), smem_of(down_stages), st, wd, am, p);
+    if (e != cudaSuccess) {
+        cudaMemsetAsync(plan->mask_count, 0, sizeof(unsigned), st);      // what the down launch would have taken back
+        return record_cuda(plan, e, "mx_down_kernel");
+    }
     plan->launches += 2;
     return CS_OK;
 }

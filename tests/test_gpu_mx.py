@@ -153,6 +153,13 @@ def test_norm_matches_definition(B, d, xt, dt):
     plan.close()
 
 
+@pytest.mark.parametrize("B,d", [(700, 5120), (2100, 4096), (400, 8192), (1300, 1152), (2500, 1024), (610, 4224), (9600, 128)])
+@pytest.mark.parametrize("xt,dt", [(torch.float32, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, None)])
+def test_norm_more_rows_than_one_round(B, d, xt, dt):
+    """CTAs that take several rows, with a ring of two to eight of them."""
+    test_norm_matches_definition(B, d, xt, dt)
+
+
 def test_norm_rows_of_zeros_nan_and_infinity():
     g = gen(2)
     x = randn(g, 6, 256)
