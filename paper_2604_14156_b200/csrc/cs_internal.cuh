@@ -70,6 +70,7 @@ struct cs_plan {
     // microscaled path (w_dtype CS_MX4; shares mask, glist and nu)
     uint8_t *mx_a;         // [max_tokens, d_ff] e4m3 SwiGLU activations over the group list
     uint8_t *mx_a_scales;  // [max_tokens / 128 tiles, G, 512]
+    int mx_clusters[9];    // clusters of 1 .. 8 CTAs that the device holds at once, a CTA to an SM
     unsigned *mx_done;     // [max_tokens / 256 + 1] what a large batch's products wait for (zero between calls)
     float *mx_partial;     // f32 parts of large batches' outputs
     float *x_host_in;  // [max_tokens, d] staging for the host-buffer entry point

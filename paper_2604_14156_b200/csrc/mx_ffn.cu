@@ -404,6 +404,16 @@ cs_status prepare_mx_ffn(cs_plan *plan) {
     for (auto *k : {mx_gateup_kernel, mx_down_kernel})
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxSmemOne) != cudaSuccess || prefer_shared(k) != cudaSuccess)
             return CS_ERR_CUDA;
+    // Clusters stand within a part of the device, so fewer of them fit than its SMs suggest (of 8 CTAs 15, not 18), and one more is another round.
+    for (int cs = 1; cs <= kMxMaxCluster; ++cs) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        cfg.gridDim = dim3(cs, 1024); cfg.blockDim = dim3(kMxThreads); cfg.dynamicSmemBytes = kMxSmemOne - 2048;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&plan->mx_clusters[cs], mx_gateup_kernel, &cfg) != cudaSuccess) return CS_ERR_CUDA;
+    }
     return prefer_shared(mx_list_kernel) == cudaSuccess ? prepare_mx_wide(plan) : CS_ERR_CUDA;
 }
 
@@ -421,7 +431,6 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     // Shared memory.  Where the weights are few (gate/up's tiles leave room for clusters of two on an SM each), one CTA of gate/up and two of down share an
     // SM, so that down's CTAs start, and load their weights, while gate/up runs; otherwise two CTAs of a product, or one where a tile has more than 128 tokens.
     const bool beside = tile <= 32 && 4 * cap <= plan->sm_count, two = !beside && tile <= 128;
-    const int slots = plan->sm_count * (two ? 2 : 1);
     auto ring = [&](int bytes) { return max(2, min(kMxMaxStages, (bytes - 1024 - (int)sizeof(MxBars) - 64) / mx_stage_bytes(tile))); };
     const int stages = ring(beside ? kMxSmemGateUp : two ? kMxSmemTwo : kMxSmemOne), down_stages = beside ? ring(kMxSmemDown) : stages;
     auto smem_of = [&](int n) { return 1024 + (size_t)max(n * mx_stage_bytes(tile), tile * kMxPitch * 4); };
@@ -445,11 +454,20 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
         plan->launches += 1;
     }
     if (wide) return launch_mx_wide(plan, L, q, p, st);
-    int cs = max(1, min(min(kMxMaxCluster, kb / 4), slots / (2 * cap)));
+    // Gate/up's clusters: as many CTAs as fill the SMs once, or, for long rows and few tokens, twice; where the k blocks that a CTA is spared (0.31 us
+    // each, 0.42 with the shorter rings beyond 64 tokens) are worth more than the exchange (1.4 us and 0.04 a token).  d = 4096, whole calls by CTAs to a cluster 1, 2, 3, 4 (8): 44 tiles, 1 token 16.9, 14.3,
+    // 13.8, 13.9 (17.9) us; 132, 3 tokens 19.4, 18.0, 23.0; 120, 16 tokens 20.0, 19.0, 24.4; 64 tokens 23.5, 24.9, 30.0; 64, 64 tokens 20.5, 18.5, 20.8, 128 tokens
+    // 26.9, 23.9.
+    // d = 2048, 96 tiles, 16 tokens 13.8, 14.3, 17.9; d = 1024, 48 tiles, 16 tokens 10.2, 10.8, 11.3.
+    int cs = max(1, min(min(kMxMaxCluster, kb / 2), plan->sm_count / (2 * cap)));
+    if (cs == 1 && tile <= 32 && 20 * cap <= 9 * plan->sm_count) cs = 2;
+    while (beside && cs > 1 && 2 * cap > plan->mx_clusters[cs]) --cs;
+    if ((tile <= 64 ? 31 : 42) * (kb - (kb + cs - 1) / cs) <= 140 + 4 * B) cs = 1;
     e = launch_clusters(mx_gateup_kernel, dim3(cs, 2 * cap), smem_of(stages), st, wg, xm, p);
     if (e != cudaSuccess) return record_cuda(plan, e, "mx_gateup_kernel");
     p.w_scales = L->down_scales; p.x_scales = plan->mx_a_scales; p.stages = down_stages;
     cs = max(1, min(min(kMxMaxCluster, cap), plan->sm_count * (beside ? 2 : 1) / kb));
+    while (!beside && cs > 1 && kb > plan->mx_clusters[cs]) --cs;
     e = launch_clusters(mx_down_kernel, dim3(cs, kb), smem_of(down_stages), st, wd, am, p);
     if (e != cudaSuccess) {
         cudaMemsetAsync(plan->mask_count, 0, sizeof(unsigned), st);      // what the down launch would have taken back
