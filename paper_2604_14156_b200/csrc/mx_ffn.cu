@@ -27,7 +27,7 @@ constexpr int kMxMaxStages = 8;
 constexpr int kMxMaxCluster = 8;
 constexpr int kMxReadyPolls = 16;
 constexpr int kMxPitch = 132;                        // floats from column to column of the spilled tile: float4 reads of 8 columns hit all banks
-constexpr int kMxNarrowTokens = 128, kMxNarrowShared = 192, kMxMaxTile = 192;   // larger batches take the pairs of mx_wide.cu, see launch_mx_ffn
+constexpr int kMxNarrowTokens = 128, kMxNarrowFew = 160, kMxMaxTile = 160;   // larger batches take the pairs of mx_wide.cu, see launch_mx_ffn
 
 struct MxBars {
     uint64_t full[kMxMaxStages], empty[kMxMaxStages], acc;
@@ -423,10 +423,10 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int cap = shared ? k : (int)min((int64_t)G, (int64_t)B * k);
     const int rows = shared ? 1 : B;
     // Which kernels.  Pairs take 256 tokens for the price of one, but a group to an item: few groups leave most pairs without one.  Narrow against wide, us:
-    // own supports, 22 of 86 groups of d = 4096, 128 tokens 40.8 and 47.0, 129 (one CTA to an SM) 50.7 and 47.0, 200 56.5 and 48.4; 6 of 24 of 1024, 128 tokens
-    // 17.4 and 20.3, 129 21.4 and 20.5; 12 of 48 of 2048, where the line is late, 64 tokens 25.0 and 23.8, 128 32.8 and 25.9.  Shared, 22 groups of
-    // 4096, 129 tokens 24.1 and 28.9, 200 28.1 and 29.3, 256 31.1 and 30.2; 54 of 5120, 160 tokens 34.7 and 36.6, 200 37.5 and 37.1.
-    const bool wide = B > (shared && 2 * cap <= plan->sm_count ? kMxNarrowShared : kMxNarrowTokens);
+    // 22 of 86 groups of d = 4096, own supports, 100 tokens 38.4 and 45.8, 128 40.7 and 46.9, 129 (one CTA to an SM) 48.9 and 46.8, 200 55.5 and 48.2.
+    // Where gate/up's tiles fit the SMs once: 16 of 60 of 4096, 144 tokens 33.9 and 33.9, 176 36.1 and 34.3; 12 of 48 of 2048 25.2 and 26.1, 28.4 and 26.5;
+    // shared, 22 of 4096 25.0 and 29.1, 26.7 and 29.0; 54 of 5120 33.2 and 36.4, 34.9 and 36.8.
+    const bool wide = B > (2 * cap <= plan->sm_count ? kMxNarrowFew : kMxNarrowTokens);
     const int tile = min(kMxMaxTile, (B + 15) / 16 * 16);
     // Shared memory.  Where the weights are few (gate/up's tiles leave room for clusters of two on an SM each), one CTA of gate/up and two of down share an
     // SM, so that down's CTAs start, and load their weights, while gate/up runs; otherwise two CTAs of a product, or one where a tile has more than 128 tokens.
@@ -455,10 +455,9 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     }
     if (wide) return launch_mx_wide(plan, L, q, p, st);
     // Gate/up's clusters: as many CTAs as fill the SMs once, or, for long rows and few tokens, twice; where the k blocks that a CTA is spared (0.31 us
-    // each, 0.42 with the shorter rings beyond 64 tokens) are worth more than the exchange (1.4 us and 0.04 a token).  d = 4096, whole calls by CTAs to a cluster 1, 2, 3, 4 (8): 44 tiles, 1 token 16.9, 14.3,
-    // 13.8, 13.9 (17.9) us; 132, 3 tokens 19.4, 18.0, 23.0; 120, 16 tokens 20.0, 19.0, 24.4; 64 tokens 23.5, 24.9, 30.0; 64, 64 tokens 20.5, 18.5, 20.8, 128 tokens
-    // 26.9, 23.9.
-    // d = 2048, 96 tiles, 16 tokens 13.8, 14.3, 17.9; d = 1024, 48 tiles, 16 tokens 10.2, 10.8, 11.3.
+    // each, 0.42 with the shorter rings beyond 64 tokens) are worth more than the exchange (1.4 us and 0.04 a token).  d = 4096, whole calls by CTAs to a
+    // cluster 1, 2, 3, 4 (8): 44 tiles, 1 token 16.9, 14.3, 13.8, 13.9 (17.9) us; 132, 3 tokens 19.4, 18.0, 23.0; 120, 16 tokens 20.0, 19.0, 24.4; 64 tokens
+    // 23.5, 24.9, 30.0; 64, 64 tokens 20.5, 18.5, 20.8, 128 tokens 26.9, 23.9.  d = 2048, 96 tiles, 16 tokens 13.8, 14.3, 17.9; d = 1024, 48 tiles, 16 tokens 10.2, 10.8, 11.3.
     int cs = max(1, min(min(kMxMaxCluster, kb / 2), plan->sm_count / (2 * cap)));
     if (cs == 1 && tile <= 32 && 20 * cap <= 9 * plan->sm_count) cs = 2;
     while (beside && cs > 1 && 2 * cap > plan->mx_clusters[cs]) --cs;
