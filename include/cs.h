@@ -382,7 +382,8 @@ cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_
  *   -> x_out [B,d] of x's type (may be x or NULL), n_out [B,d] f32 or NULL (what cs_sketch reads), q [B,d] e4m3 bytes,
  *   s [ceil(B/128), d/128, 512] bytes: the scale of row r, block b at byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of tile
  *   (r / 128, b / 4), the order in which block-scaled tensor-core products read scales; scales of rows from B on are 0.
- * A NaN makes its row NaN, an infinity its block (the rest of such a row is 0); rows keep to themselves.  Other than x_out = x, outputs overlap no input.
+ * Magnitudes up to 2^60 (the sum of squares is formed in f32 by parts).  A NaN makes its row NaN, an infinity its block (the
+ * rest of such a row is 0); rows keep to themselves.  Other than x_out = x, outputs overlap no input.
  * Pointers are 16-byte aligned.  No scratch of the plan is used.
  */
 cs_status cs_mx_norm(cs_plan *plan, const void *x, int32_t x_dtype, const void *delta, int32_t delta_dtype, const float *gamma,

@@ -7,11 +7,17 @@
 //
 // Both products are tcgen05.mma kind::mxf8f6f4 with block scales: the tensor core multiplies the two block scales into every partial product of 32
 // and adds in f32, so neither operand is ever widened.  Weights are the M side: a tile is 128 rows x 128 columns, 8 KB in memory and 16 KB in
-// shared memory (TMA spreads 16 codes over 16 bytes, the form the instruction wants).  Tokens are the N side, 16 to 256 columns.  In
+// shared memory (TMA spreads 16 codes over 16 bytes, the form the instruction wants).  Tokens are the N side, 16 to 160 columns.  In
 // gate/up 64 channels of W_gate and the same 64 of W_up share a tile: one accumulator holds both, and 172 tiles for 86 groups spread better over
 // 148 SMs than 86.  The scales go from shared memory to tensor memory with tcgen05.cp, in a place of their own per stage of the ring.
 //
-// Work is split over a cluster where there are fewer tiles than SMs can hold: each CTA of a cluster takes a part of the k blocks, and the
+// What bounds it: HBM's 6.5 TB/s want 42 KB of weights in flight on every SM (a load takes 0.4 us from L2 and 0.9 from HBM, and 0.6 pass from the
+// end of a stage's products to the next load's issue and back), and weights take twice their size in shared memory: four stages of 25 KB, two CTAs to an SM
+// where there are that many, stream 5.0 TB/s at 64 tokens.  At one token the chain of latencies is all there is: list, first loads, products, exchange,
+// and again.  (Two warps issuing the products, loads asked of L2 ahead of the ring, one CTA with eight stages, and waits that poll gained nothing.)  7B layer, 22 of 86 groups: 1 token 13.1
+// us, 3 tokens 17.5, 64 tokens 28.6, against 18.4, 48.6 and 72.3 MB of weights.
+//
+// Work is split over a cluster where there are fewer tiles than SMs: each CTA of a cluster takes a part of the k blocks, and the
 // accumulators are added over distributed shared memory in a fixed order.
 #include <stdio.h>
 
@@ -313,9 +319,8 @@ mx_gateup_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant
                 const uint32_t other = __shfl_down_sync(0xffffffffu, byte, 2);
                 if (in) {
                     *reinterpret_cast<uint4 *>(p.a + (size_t)c * p.cap * 128 + entry * 128 + half * 64 + part * 16) = make_uint4(o[0], o[1], o[2], o[3]);
-                    if (part == 0)
-                        *reinterpret_cast<uint16_t *>(p.a_scales + ((size_t)(c >> 7) * p.cap + entry) * kMxTileBytes + (c & 31) * 16 + ((c & 127) >> 5) * 4 + half * 2) =
-                            (uint16_t)(byte | other << 8);
+                    uint8_t *to = p.a_scales + ((size_t)(c >> 7) * p.cap + entry) * kMxTileBytes + (c & 31) * 16 + ((c & 127) >> 5) * 4 + half * 2;
+                    if (part == 0) *reinterpret_cast<uint16_t *>(to) = (uint16_t)(byte | other << 8);
                 }
             }
         }
@@ -457,7 +462,8 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     // Gate/up's clusters: as many CTAs as fill the SMs once, or, for long rows and few tokens, twice; where the k blocks that a CTA is spared (0.31 us
     // each, 0.42 with the shorter rings beyond 64 tokens) are worth more than the exchange (1.4 us and 0.04 a token).  d = 4096, whole calls by CTAs to a
     // cluster 1, 2, 3, 4 (8): 44 tiles, 1 token 16.9, 14.3, 13.8, 13.9 (17.9) us; 132, 3 tokens 19.4, 18.0, 23.0; 120, 16 tokens 20.0, 19.0, 24.4; 64 tokens
-    // 23.5, 24.9, 30.0; 64, 64 tokens 20.5, 18.5, 20.8, 128 tokens 26.9, 23.9.  d = 2048, 96 tiles, 16 tokens 13.8, 14.3, 17.9; d = 1024, 48 tiles, 16 tokens 10.2, 10.8, 11.3.
+    // 23.5, 24.9, 30.0; 64, 64 tokens 20.5, 18.5, 20.8, 128 tokens 26.9, 23.9.  d = 2048, 96 tiles, 16 tokens 13.8, 14.3,
+    // 17.9; d = 1024, 48 tiles, 16 tokens 10.2, 10.8, 11.3.
     int cs = max(1, min(min(kMxMaxCluster, kb / 2), plan->sm_count / (2 * cap)));
     if (cs == 1 && tile <= 32 && 20 * cap <= 9 * plan->sm_count) cs = 2;
     while (beside && cs > 1 && 2 * cap > plan->mx_clusters[cs]) --cs;

@@ -296,8 +296,8 @@ cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *
         using TX = decltype(tx);
         using TD = decltype(td);
         if (stay)
-            e = launch_pdl(true, each == 4 ? mx_norm_rows_kernel<TX, TD, 4> : each == 2 ? mx_norm_rows_kernel<TX, TD, 2> : mx_norm_rows_kernel<TX, TD, 1>, dim3(ctas * plan->sm_count), dim3(threads),
-                           (size_t)stages * row_bytes, st, static_cast<const TX *>(x), static_cast<const TD *>(delta), gamma, B, d, 1. / d, plan->cfg.rms_eps,
+            e = launch_pdl(true, each == 4 ? mx_norm_rows_kernel<TX, TD, 4> : each == 2 ? mx_norm_rows_kernel<TX, TD, 2> : mx_norm_rows_kernel<TX, TD, 1>,
+                           dim3(ctas * plan->sm_count), dim3(threads), (size_t)stages * row_bytes, st, static_cast<const TX *>(x), static_cast<const TD *>(delta), gamma, B, d, 1. / d, plan->cfg.rms_eps,
                            static_cast<TX *>(x_out), n_out, q, s, stages, plan->status);
         else
             e = launch_pdl(true, mx_norm_kernel<TX, TD>, dim3(B + (B % 128 != 0 ? 4 : 0)), block, 0, st, static_cast<const TX *>(x),

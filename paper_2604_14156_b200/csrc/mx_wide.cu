@@ -1,8 +1,8 @@
 // The FFN on microscaled operands for batches beyond one tile of mx_ffn.cu and for prompts, on pairs of CTAs.
 //
-//   mx_wide_kernel<false, 4>  gate/up: an item is 256 tokens x one group (128 channels of W_gate and of W_up)
-//   mx_wide_kernel<true, .>  down: an item is 256 tokens x 256 (or 192) columns of the output, or a part of the list of it
-//   mx_wide_sum_kernel      adds the parts
+//   mx_wide_kernel      both products: first every gate/up item (256 tokens x one group: 128 channels of W_gate and of W_up), then every down item (256
+//                       tokens x 256 or 192 columns of the output, or a part of the list of it)
+//   mx_wide_sum_kernel  adds the parts
 //
 // Here the tensor pipe is the bound, and before it what an SM can draw from L2: a single CTA of 128 weight rows x 256 tokens takes 41 KB for 512
 // cycles of products.  A cluster of two CTAs issues one instruction of 256 x 256 (cta_group::2): each brings 128 tokens and 128 weight
@@ -10,8 +10,15 @@
 // block of channels: the epilogue finds a block's largest element, silu's two factors and the bytes it writes in one thread's registers.  A packed
 // gate/up tile (64 rows of W_gate, the same 64 of W_up) is one CTA's half of the columns.
 //
-// The kernel is persistent, one pair of CTAs on two SMs, and the ring of loads runs on across items.  One accumulator of 256 columns (the scales need some of
-// the other 256): the epilogue takes it into registers, 128 a thread, hands it back, and does its arithmetic while the next item's products run.
+// The kernel is persistent, one pair of CTAs on two SMs, pair i taking items i, i + pairs, ..., and the ring of loads runs on across items.  One accumulator
+// of 256 columns (the scales need some of the other 256): the epilogue takes it into registers, 128 a thread, hands it back, and does its arithmetic while the
+// next item's products run.  A down item's token loads wait until the epilogues of its token tile's gate/up items have counted themselves; its weights do
+// not.  Gate/up items wait for nothing, and a pair has done all of its own before its first down item, so every wait ends once every pair has
+// run; all waits are bounded besides.  The gate/up phase also asks L2 for the down weights.
+//
+// 2048 tokens of d = 5120, 27 of 108 groups (217 GFLOP): two launches of single CTAs 160 us, pairs 103, without spilled accumulators and with the union of the
+// supports inside the launch 83, one launch 79 (2.75 PFLOP/s; 90 over a second of load, at the clocks of the power cap).  An item's 40 k blocks take 12 us, of
+// which the products alone are 10.7, and 1 to 1.5 us pass from its last product to the next item's first.
 #include <stdio.h>
 
 #include "mx_core.cuh"
