@@ -9,7 +9,7 @@ namespace cs {
 // What a launch needs to know beside its tensor maps.
 struct MxArgs {
     const uint8_t *w_scales, *x_scales;
-    const int32_t *support;         // fold: [B, k] or, without mask, [k]
+    const int32_t *support;         // [B, k], or with `shared` [k]
     int32_t *list, *count;          // groups of the union, ascending
     unsigned *ready;                // set while a call's list stands, before its gate/up is complete
     const uint32_t *mask;           // [B, 4] membership bits, unless folded
@@ -20,10 +20,10 @@ struct MxArgs {
     int cap;                        // groups the list can hold: pitch of a and its scales
     int tile, stages;               // tokens of a tile, ring stages
     int entries;                    // of the support
-    int shared, fold;               // one support for all tokens; gate/up makes the list
+    int shared, fold;               // one support for all tokens; the products' launch makes the list, else mx_list_kernel has
 };
 
-// A batch on CTA pairs (mx_wide.cu); the list stands in p.list unless p.fold.
+// A batch on CTA pairs (mx_wide.cu).
 cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const MxArgs &p, cudaStream_t st);
 cs_status prepare_mx_wide(cs_plan *plan);
 
@@ -100,6 +100,11 @@ __device__ __forceinline__ bool mx_wait(uint64_t *bar, uint32_t parity, uint32_t
     *reinterpret_cast<volatile uint32_t *>(aborted) = 1;
     atomicCAS(&status->code, 0, (int)CS_ERR_TIMEOUT);
     return false;
+}
+// After a wait that gave up: copies may still be on their way into this CTA's shared memory; they land within microseconds.
+__device__ __forceinline__ void mx_settle(const uint32_t *aborted) {
+    if (*reinterpret_cast<const volatile uint32_t *>(aborted))
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

@@ -14,8 +14,8 @@
 // What bounds it: HBM's 6.5 TB/s want 42 KB of weights in flight on every SM (a load takes 0.4 us from L2 and 0.9 from HBM, and 0.6 pass from the
 // end of a stage's products to the next load's issue and back), and weights take twice their size in shared memory: four stages of 25 KB, two CTAs to an SM
 // where there are that many, stream 5.0 TB/s at 64 tokens.  At one token the chain of latencies is all there is: list, first loads, products, exchange,
-// and again.  (Two warps issuing the products, loads asked of L2 ahead of the ring, one CTA with eight stages, and waits that poll gained nothing.)  7B layer, 22 of 86 groups: 1 token 13.1
-// us, 3 tokens 17.5, 64 tokens 28.6, against 18.4, 48.6 and 72.3 MB of weights.
+// and again.  (Two warps issuing the products, loads asked of L2 ahead of the ring, one CTA with eight stages, and waits that poll gained nothing.)
+// 7B layer, 22 of 86 groups: 1 token 13.1 us, 3 tokens 17.5, 64 tokens 28.6, against 18.4, 48.6 and 72.3 MB of weights.
 //
 // Work is split over a cluster where there are fewer tiles than SMs: each CTA of a cluster takes a part of the k blocks, and the
 // accumulators are added over distributed shared memory in a fixed order.
@@ -229,6 +229,7 @@ __device__ __forceinline__ uint8_t *mx_setup(MxBars *bars, int stages, int cols,
     return reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
 }
 __device__ __forceinline__ void mx_teardown(MxBars *bars, int cols) {
+    mx_settle(&bars->aborted);
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x >> 5 == 1) {

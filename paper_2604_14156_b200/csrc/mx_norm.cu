@@ -248,7 +248,10 @@ mx_norm_rows_kernel(const TX *x, const TD *delta, const float *__restrict__ gamm
         }
         sum = warp_sum(sum);
         if ((t & 31) == 0) bars.part[turn][t >> 5] = sum;
-        if (!__syncthreads_and(ok)) return;      // a wait gave up: the status word says so
+        if (!__syncthreads_and(ok)) {      // a wait gave up: the status word says so
+            mx_settle(&bars.aborted);
+            return;
+        }
         if (t == 0 && row + stages * step < B) fetch(row + stages * step, ring.stage);
         sum = warp_sum((t & 31) < (int)(blockDim.x >> 5) ? bars.part[turn][t & 31] : 0.);
         const RowScale rstd = row_scale(sum, per, eps);
@@ -297,8 +300,9 @@ cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *
         using TD = decltype(td);
         if (stay)
             e = launch_pdl(true, each == 4 ? mx_norm_rows_kernel<TX, TD, 4> : each == 2 ? mx_norm_rows_kernel<TX, TD, 2> : mx_norm_rows_kernel<TX, TD, 1>,
-                           dim3(ctas * plan->sm_count), dim3(threads), (size_t)stages * row_bytes, st, static_cast<const TX *>(x), static_cast<const TD *>(delta), gamma, B, d, 1. / d, plan->cfg.rms_eps,
-                           static_cast<TX *>(x_out), n_out, q, s, stages, plan->status);
+                           dim3(ctas * plan->sm_count), dim3(threads), (size_t)stages * row_bytes, st, static_cast<const TX *>(x),
+                           static_cast<const TD *>(delta), gamma, B, d, 1. / d, plan->cfg.rms_eps, static_cast<TX *>(x_out), n_out, q, s, stages,
+                           plan->status);
         else
             e = launch_pdl(true, mx_norm_kernel<TX, TD>, dim3(B + (B % 128 != 0 ? 4 : 0)), block, 0, st, static_cast<const TX *>(x),
                            static_cast<const TD *>(delta), gamma, B, d, 1. / d, plan->cfg.rms_eps, static_cast<TX *>(x_out), n_out, q, s);

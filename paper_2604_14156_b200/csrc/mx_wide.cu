@@ -355,6 +355,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     }
 done:
     __syncwarp();
+    mx_settle(&bars.aborted);
     // Neither CTA leaves (or frees tensor memory) while the other may still read its shared memory or signal its barriers; every wait above
     // is bounded, so both reach this point.
     tc_fence_before();

@@ -280,6 +280,18 @@ def test_ffn_rows_behind_the_batch_stay_and_scratch_is_reused():
     p.plan.close()
 
 
+@pytest.mark.parametrize("B", [40, 300, 2000])
+def test_ffn_output_on_a_16_byte_boundary(B):
+    p = Problem(B, 640, 12, 5, False)
+    out = torch.full((B * 640 + 16,), 3.0, dtype=torch.bfloat16, device=DEV)
+    rows = out[8:8 + B * 640].view(B, 640)
+    assert rows.data_ptr() % 32 == 16
+    assert torch.equal(p.run(out=rows), p.run())
+    p.check(rows)
+    assert (out[:8] == 3).all() and (out[-8:] == 3).all()
+    p.plan.close()
+
+
 def test_ffn_scales_of_padding_rows_may_be_anything():
     p = Problem(20, 256, 6, 2, False)
     want = p.run()
