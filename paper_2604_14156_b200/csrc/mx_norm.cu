@@ -67,7 +67,7 @@ __device__ __forceinline__ void finish_chunk(float (&h)[8], const float (&g)[8],
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         n[j] = h[j] * r.hi * g[j];
-        near |= ((__float_as_uint(n[j]) + 4) & 0x7ffff) <= 8;
+        near |= ((__float_as_uint(n[j]) + 4) & 0x7ffff) <= 8 && n[j] != 0.f;      // (zeros are exact, and sums of bf16 are often zero)
     }
     const size_t at = (size_t)row * d + c * 8;
     if (n_out != nullptr && in) store_row8(n_out + at, n);
