@@ -123,7 +123,7 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
         alloc((void **)&p->mx_a_scales, (nt + 127) / 128 * p->G * kMxTileBytes);
         alloc((void **)&p->mx_done, ((nt + 255) / 256 + 1) * sizeof(unsigned));
         if (e == cudaSuccess) e = cudaMemset(p->mx_done, 0, ((nt + 255) / 256 + 1) * sizeof(unsigned));
-        alloc((void **)&p->mx_partial, mx_wide_partial_bytes(p));
+        if (mx_wide_partial_bytes(p) != 0) alloc((void **)&p->mx_partial, mx_wide_partial_bytes(p));
     } else {
         alloc((void **)&p->x_host_in, nt * cfg->d * sizeof(float));
         alloc((void **)&p->x_host_out, nt * cfg->d * sizeof(float));

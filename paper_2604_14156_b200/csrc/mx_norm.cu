@@ -3,7 +3,7 @@
 // A row is one pass of one CTA, eight elements a thread, kept in registers between the sum of squares and the quantisation, so HBM sees every byte
 // once.  mx_norm_kernel is a CTA per row: one round of latencies, for as many rows as are
 // resident at once.  More rows take mx_norm_rows_kernel, whose CTAs stay and have the next rows' bulk copies in flight while they work on one: with a CTA
-// per row the loads wait for the row before (2048 rows of 5120 bf16 took 21.5 us; now 19.3, 3.8 TB/s, the bound being instructions).
+// per row the loads wait for the row before (2048 rows of 5120 bf16 took 21.5 us; now 18.9, 3.9 TB/s, the bound being instructions).
 #include "mx_core.cuh"
 
 namespace cs {

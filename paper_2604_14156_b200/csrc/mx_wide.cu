@@ -414,7 +414,9 @@ cs_status prepare_mx_wide(cs_plan *plan) {
     return prefer_shared(mx_wide_sum_kernel) == cudaSuccess ? CS_OK : CS_ERR_CUDA;
 }
 
-size_t mx_wide_partial_bytes(const cs_plan *plan) { return (size_t)(plan->sm_count / 2) * kWideTokens * 256 * sizeof(float); }
+size_t mx_wide_partial_bytes(const cs_plan *plan) {      // plans of small batches never come here
+    return plan->cfg.max_tokens <= 128 ? 0 : (size_t)(plan->sm_count / 2) * kWideTokens * 256 * sizeof(float);
+}
 
 cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const MxArgs &args, cudaStream_t st) {
     const int d = args.d, kb = d / 128, G = args.G, B = args.B, chunks = (B + 127) / 128, pairs = plan->sm_count / 2;
