@@ -584,12 +584,19 @@ def cs_mx_quantize(w, transpose: bool = False, codes=None, scales=None, stream=N
     ptr, ld = _matrix(w, _FLOATS, "w", device)
     rows, cols = w.shape
     n, nb = (cols, -(-rows // 32)) if transpose else (rows, -(-cols // 32))
-    t = _outputs(_matrix_templates, (n, nb, device), w.device, ((n, 16 * nb), torch.uint8), ((n, nb), _E8M0))
-    codes = _empty_like(t[0]) if codes is None else codes
-    scales = _empty_like(t[1]) if scales is None else scales
-    st = lib.cs_mx_quantize(ptr, _DTYPES[w.dtype], rows, cols, ld, 1 if transpose else 0,
-                            _checked(codes, (torch.uint8,), "codes", (n, 16 * nb), device),
-                            _checked(scales, _BYTES, "scales", (n, nb), device), _stream(stream))
+    if codes is None or scales is None:
+        t = _outputs(_matrix_templates, (n, nb, device), w.device, ((n, 16 * nb), torch.uint8), ((n, nb), _E8M0))
+    if codes is None:
+        codes = _empty_like(t[0])
+        pc = codes.data_ptr()
+    else:
+        pc = _checked(codes, (torch.uint8,), "codes", (n, 16 * nb), device)
+    if scales is None:
+        scales = _empty_like(t[1])
+        ps = scales.data_ptr()
+    else:
+        ps = _checked(scales, _BYTES, "scales", (n, nb), device)
+    st = lib.cs_mx_quantize(ptr, _DTYPES[w.dtype], rows, cols, ld, 1 if transpose else 0, pc, ps, _stream(stream))
     if st != 0:
         raise CSError(st, "cs_mx_quantize")
     return codes, scales
@@ -600,14 +607,18 @@ def cs_mx_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, s
     lib = _lib or load_library()
     device = _device_index()
     rows, nb = codes.shape[0], -(-cols // 32)
+    pc = _checked(codes, (torch.uint8,), "codes", (rows, 16 * nb), device)
+    ps = _checked(scales, _BYTES, "scales", (rows, nb), device)
     if out is None:
+        if dtype not in _FLOATS:
+            raise TypeError(f"dtype must be one of {', '.join(map(str, _FLOATS))}, got {dtype}")
         out = _empty_like(_outputs(_matrix_templates, (rows, cols, dtype, device), codes.device, ((rows, cols), dtype))[0])
-    ptr, ld = _matrix(out, _FLOATS, "out", device)
-    if out.shape != (rows, cols):
-        raise ValueError(f"out must have shape {(rows, cols)}, got {tuple(out.shape)}")
-    st = lib.cs_mx_dequantize(_checked(codes, (torch.uint8,), "codes", (rows, 16 * nb), device),
-                              _checked(scales, _BYTES, "scales", (rows, nb), device), rows, cols, _DTYPES[out.dtype], ptr, ld,
-                              _stream(stream))
+        ptr, ld = out.data_ptr(), cols
+    else:
+        ptr, ld = _matrix(out, _FLOATS, "out", device)
+        if out.shape != (rows, cols):
+            raise ValueError(f"out must have shape {(rows, cols)}, got {tuple(out.shape)}")
+    st = lib.cs_mx_dequantize(pc, ps, rows, cols, _DTYPES[out.dtype], ptr, ld, _stream(stream))
     if st != 0:
         raise CSError(st, "cs_mx_dequantize")
     return out
