@@ -675,14 +675,16 @@ def cs_mx_norm(plan: Plan, x, gamma=None, delta=None, want_n: bool = False, x_ou
 def _mx_ffn(call, name, plan: Plan, layer: MxLayer, q, s, support, support_shape, out, stream):
     B, d = q.shape[0], plan.d
     device = _device_index()
+    # before the output: a template made for a tensor of another device would serve the calls after this one
+    pq = _checked(q, _BYTES, "q", (B, d), device)
+    ps = _checked(s, _BYTES, "s", (-(-B // 128), d // 128, 32, 4, 4), device)
+    pi = _checked(support, (torch.int32,), "support", support_shape, device)
     if out is None:
         out = _empty_like(_outputs(plan._templates, ("ffn", B, device), q.device, ((B, d), torch.bfloat16))[0])
         po = out.data_ptr()
     else:
         po = _checked(out, (torch.bfloat16,), "out", (B, d), device)
-    st = call(plan.handle, layer.ref, _checked(q, _BYTES, "q", (B, d), device),
-              _checked(s, _BYTES, "s", (-(-B // 128), d // 128, 32, 4, 4), device),
-              _checked(support, (torch.int32,), "support", support_shape, device), B, po, _stream(stream))
+    st = call(plan.handle, layer.ref, pq, ps, pi, B, po, _stream(stream))
     if st != 0:
         plan.check(st, name)
     return out

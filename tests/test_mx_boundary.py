@@ -71,3 +71,39 @@ def test_binding_refuses_cpu_and_foreign_types():
     assert binding._checked(None, binding._BYTES, "q", (4,), 0, True) is None
     with pytest.raises(TypeError):
         binding._dtype_code(torch.zeros(4, dtype=torch.float16), "x")
+
+
+class _HostPlan:
+    """What the binding itself looks at of a plan."""
+
+    def __init__(self, d=256, k=2):
+        self.d, self.k, self.device, self._templates = d, k, 0, {}
+
+        def call(*args):
+            raise AssertionError("a refused call reached the library")
+        self.lib = type("lib", (), dict(cs_mx_ffn=call, cs_mx_ffn_shared=call, cs_mx_norm=call))
+        self.handle = None
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_refused_ffn_call_leaves_no_output_template(monkeypatch, shared):
+    """The next call would allocate its output from it, on the refused tensor's device."""
+    monkeypatch.setattr(binding, "_device_index", lambda: 0)
+    plan, layer = _HostPlan(), type("layer", (), dict(ref=None))
+    q = torch.zeros((8, 256), dtype=torch.float8_e4m3fn)
+    s = torch.zeros((1, 2, 32, 4, 4), dtype=torch.float8_e8m0fnu)
+    support = torch.zeros((2,) if shared else (8, 2), dtype=torch.int32)
+    with pytest.raises((TypeError, ValueError)):
+        (binding.cs_mx_ffn_shared if shared else binding.cs_mx_ffn)(plan, layer, q, s, support)
+    assert plan._templates == {}
+
+
+def test_refused_norm_and_matrix_calls_leave_no_output_template(monkeypatch):
+    monkeypatch.setattr(binding, "_device_index", lambda: 0)
+    plan, before = _HostPlan(), dict(binding._matrix_templates)
+    x, codes = torch.zeros((8, 256)), torch.zeros((8, 128), dtype=torch.uint8)
+    for call in (lambda: binding.cs_mx_norm(plan, x), lambda: binding.cs_mx_quantize(x),
+                 lambda: binding.cs_mx_dequantize(codes, torch.zeros((8, 8), dtype=torch.uint8), 256)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    assert plan._templates == {} and binding._matrix_templates == before
