@@ -121,8 +121,8 @@ cs_status cs_plan_create(const cs_config *cfg, cs_plan **out) {
     if (mx) {
         alloc((void **)&p->mx_a, nt * cfg->d_ff);
         alloc((void **)&p->mx_a_scales, (nt + 127) / 128 * p->G * kMxTileBytes);
-        alloc((void **)&p->mx_done, ((nt + 255) / 256 + 1) * sizeof(unsigned));
-        if (e == cudaSuccess) e = cudaMemset(p->mx_done, 0, ((nt + 255) / 256 + 1) * sizeof(unsigned));
+        alloc((void **)&p->mx_done, mx_done_bytes(p));
+        if (e == cudaSuccess) e = cudaMemset(p->mx_done, 0, mx_done_bytes(p));
         if (mx_wide_partial_bytes(p) != 0) alloc((void **)&p->mx_partial, mx_wide_partial_bytes(p));
     } else {
         alloc((void **)&p->x_host_in, nt * cfg->d * sizeof(float));

@@ -71,7 +71,7 @@ struct cs_plan {
     uint8_t *mx_a;         // [max_tokens, d_ff] e4m3 SwiGLU activations over the group list
     uint8_t *mx_a_scales;  // [max_tokens / 128 tiles, G, 512]
     int mx_clusters[9];    // clusters of 1 .. 8 CTAs that the device holds at once, a CTA to an SM
-    unsigned *mx_done;     // [max_tokens / 256 + 1] what a large batch's products wait for (zero between calls)
+    unsigned *mx_done;     // what a large batch's products claim and wait for (zero between calls; mx_done_bytes)
     float *mx_partial;     // f32 parts of large batches' outputs
     float *x_host_in;  // [max_tokens, d] staging for the host-buffer entry point
     float *x_host_out; // [max_tokens, d]

@@ -79,6 +79,8 @@ cs_status launch_mx_norm(cs_plan *plan, const void *x, int x_dtype, const void *
                          void *x_out, float *n_out, uint8_t *q, uint8_t *s, cudaStream_t st);
 // mx_ffn.cu: support [B, k], or with `shared` [k]
 cs_status prepare_mx_ffn(cs_plan *plan);
+constexpr int kMxDoneOffset = 32;                    // mx_done: the next item in a line of its own, then a count for each token tile, then one of pairs
+inline size_t mx_done_bytes(const cs_plan *plan) { return (kMxDoneOffset + ((size_t)plan->cfg.max_tokens + 255) / 256 + 1) * sizeof(unsigned); }
 size_t mx_wide_partial_bytes(const cs_plan *plan);   // mx_wide.cu's scratch for parts of an output
 cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, const uint8_t *s, const int32_t *support, bool shared,
                         int B, void *out, cudaStream_t st);

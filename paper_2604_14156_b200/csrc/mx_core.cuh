@@ -88,12 +88,18 @@ struct MxRing {
         if (++stage == stages) { stage = 0; phase ^= 1; }
     }
 };
+// PEER: what the barrier stands for was written, or read, by the other CTA of a pair.
+template <bool PEER = false>
 __device__ __forceinline__ bool mx_wait(uint64_t *bar, uint32_t parity, uint32_t *aborted, DeviceStatus *status) {
     const uint32_t addr = smem_u32(bar);
     for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+        if (PEER)
+            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+        else
+            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(done) : "r"(addr), "r"(parity) : "memory");
         if (done) return true;
         if (*reinterpret_cast<volatile uint32_t *>(aborted)) return false;
     }

@@ -10,11 +10,13 @@
 // block of channels: the epilogue finds a block's largest element, silu's two factors and the bytes it writes in one thread's registers.  A packed
 // gate/up tile (64 rows of W_gate, the same 64 of W_up) is one CTA's half of the columns.
 //
-// The kernel is persistent, one pair of CTAs on two SMs, pair i taking items i, i + pairs, ..., and the ring of loads runs on across items.  One accumulator
-// of 256 columns (the scales need some of the other 256): the epilogue takes it into registers, 128 a thread, hands it back, and does its arithmetic while the
+// The kernel is persistent, one pair of CTAs on two SMs.  Pairs claim items in order from a counter, the next one shortly before the loads of the last
+// end (not earlier, so that pairs that start first leave items to the others), and the ring of loads runs on across items.  One accumulator of 256
+// columns (the scales need some of the other 256): the epilogue takes it into registers, 128 a thread, hands it back, and does its arithmetic while the
 // next item's products run.  A down item's token loads wait until the epilogues of its token tile's gate/up items have counted themselves; its weights do
-// not.  Gate/up items wait for nothing, and a pair has done all of its own before its first down item, so every wait ends once every pair has
-// run; all waits are bounded besides.  The gate/up phase also asks L2 for the down weights.
+// not.  Gate/up items wait for nothing, come first in the order of claims, and are claimed by pairs that run; so every wait ends however few of the
+// pairs the device has room for (items dealt out in advance would wait for pairs that have no SM yet).  All waits are bounded besides.  The gate/up
+// phase also asks L2 for the down weights.
 //
 // 2048 tokens of d = 5120, 27 of 108 groups (217 GFLOP): two launches of single CTAs 160 us, pairs 103, without spilled accumulators and with the union of the
 // supports inside the launch 83, one launch 79 (2.75 PFLOP/s; 90 over a second of load, at the clocks of the power cap).  An item's 40 k blocks take 12 us, of
@@ -30,8 +32,11 @@ namespace {
 constexpr int kWideStages = 6;
 constexpr int kWideStageBytes = 128 * 128 + kMxWBytes + 3 * kMxTileBytes + 512;     // tokens, weights, scales: a multiple of 1024
 constexpr int kWideEpiWarps = 8;
-constexpr int kWideThreads = 128 + 32 * kWideEpiWarps;    // token loads, products, weight loads, one idle warp; epilogue
+constexpr int kWideThreads = 128 + 32 * kWideEpiWarps;    // token loads, products, weight loads, claims and the support's check; epilogue
 constexpr int kWideTokens = 256;
+constexpr int kWideClaims = 2;      // items a pair has claimed and not all of its warps have taken up
+constexpr int kWideAhead = 8;       // k blocks (0.27 us each) before the end of an item's loads at which the next is claimed (1 to 1.5 us)
+constexpr int kWideTakers = 2 * (2 + kWideEpiWarps) + 1;      // loads and epilogue of both CTAs, products of one
 static_assert(kWideStageBytes % 1024 == 0, "operands stand on 1024-byte boundaries");
 
 struct WideArgs {
@@ -42,10 +47,12 @@ struct WideArgs {
     const uint8_t *down_codes, *down_scales;
     float *partial;    // [down item and part][256 tokens][256 columns]
     unsigned *done;    // [ztiles] epilogue warps that have stored their part of a token tile's activations; behind them the pairs that have ended
+    unsigned *next;    // the next item; not in a line of `done`, which waiting pairs poll
 };
 
 struct WideBars {
-    uint64_t full[kWideStages], empty[kWideStages], acc_full, acc_empty;
+    uint64_t full[kWideStages], empty[kWideStages], acc_full, acc_empty, claim_ask, claim_full[kWideClaims], claim_empty[kWideClaims];
+    int claim[kWideClaims];
     uint32_t tmem, aborted;
     uint32_t all[4];
     int32_t list[kMaxG], count;
@@ -115,6 +122,46 @@ __device__ __forceinline__ bool wide_ready(const unsigned *done, unsigned need, 
     return false;
 }
 
+// The pair's claims: one thread of its first CTA takes the next item when its token loads ask for it, and tells both CTAs, until there is none.  (Asynchronous
+// stores that the barrier counts, so that nothing has to be released: 1 us a call against a store and an arrival.)
+__device__ __forceinline__ void wide_tell(WideBars *bars, int slot, int item) {
+#pragma unroll
+    for (int cta = 0; cta < 2; ++cta) {
+        const uint32_t bar = map_to_cta(smem_u32(&bars->claim_full[slot]), cta);
+        asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], 4;" ::"r"(bar) : "memory");
+        asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+                     ::"r"(map_to_cta(smem_u32(&bars->claim[slot]), cta)), "r"(item), "r"(bar) : "memory");
+    }
+}
+__device__ __forceinline__ void wide_claim(WideBars *bars, unsigned *next, int first, int items, DeviceStatus *status) {
+    if (first >= items) return;      // told while the list was made
+    MxRing ring;
+    for (int n = 1;; ++n) {
+        ring.next(kWideClaims);
+        if (!mx_wait(&bars->claim_ask, (n - 1) & 1, &bars->aborted, status)) return;
+        if (n >= kWideClaims && !mx_wait<true>(&bars->claim_empty[ring.stage], ring.phase ^ 1, &bars->aborted, status)) return;
+        const int item = (int)atomicAdd(next, 1u);
+        wide_tell(bars, ring.stage, item);
+        if (item >= items) return;
+    }
+}
+// An arrival without release, which would hold the thread until its loads and stores, or the tensor core, have got that far: at 300 tokens of the 7B layer
+// 10 us.  `read`: what was read before and may be overwritten after it, not negative; the address takes its sign, so that the arrival cannot go ahead.
+__device__ __forceinline__ void wide_arrive(uint64_t *bar, int read) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(smem_u32(bar), 0) + (uint32_t)(read >> 31)) : "memory");
+}
+// The next item for one of the roles, a thread or with WARP a warp; `items` or more: there is none, or a wait gave up.
+template <bool WARP> __device__ __forceinline__ int wide_next(WideBars *bars, MxRing &ring, DeviceStatus *status) {
+    bool ok = mx_wait<true>(&bars->claim_full[ring.stage], ring.phase, &bars->aborted, status);
+    if (WARP) ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return 0x7fffffff;
+    const int item = *reinterpret_cast<volatile int *>(&bars->claim[ring.stage]);
+    if (WARP) __syncwarp();
+    if (!WARP || (threadIdx.x & 31) == 0) wide_arrive(&bars->claim_empty[ring.stage], item);
+    ring.next(kWideClaims);
+    return item;
+}
+
 template <int DB> __global__ void __launch_bounds__(kWideThreads, 1)
 mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_xs, const __grid_constant__ CUtensorMap tm_gu,
                const __grid_constant__ CUtensorMap tm_gus, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_as,
@@ -130,6 +177,8 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         for (int s = 0; s < kWideStages; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
         mbar_init(&bars.acc_full, 1);
         mbar_init(&bars.acc_empty, 2 * kWideEpiWarps);
+        mbar_init(&bars.claim_ask, 1);
+        for (int s = 0; s < kWideClaims; ++s) { mbar_init(&bars.claim_full[s], 1); mbar_init(&bars.claim_empty[s], kWideTakers); }
         bars.aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (const CUtensorMap *m : {&tm_x, &tm_xs, &tm_gu, &tm_gus, &tm_a, &tm_as, &tm_d, &tm_ds})
@@ -145,6 +194,9 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     tc_fence_after();
     pdl_wait();
     pdl_launch_dependents();
+    const bool claimer = rank == 0 && threadIdx.x == 96;
+    unsigned first = 0;
+    if (claimer) first = atomicAdd(w.next, 1u);      // on its way while the list is made
     if (p.fold) {
         if (threadIdx.x < 4) bars.all[threadIdx.x] = 0;
         __syncthreads();
@@ -155,17 +207,22 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
         if (threadIdx.x == 0) bars.count = ld_dep(p.count);
         if (threadIdx.x < kMaxG) bars.list[threadIdx.x] = ld_dep(p.list + threadIdx.x);
     }
+    if (claimer) wide_tell(&bars, 0, (int)first);
     __syncthreads();
     const int kb = p.d >> 7, count = bars.count, items = w.ztiles * (count + wide_across<DB>(p.d) * w.splits);
 
     if (warp == 0) {          // tokens, and the bytes both CTAs will bring
         if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
-            MxRing ring;
+            MxRing ring, claims;
             int fill = 0, ready = -1;
-            for (int i = pair; i < items; i += pairs) {
+            for (int i; (i = wide_next<false>(&bars, claims, p.status)) < items;) {
                 const WideItem t = wide_item<DB>(w, count, i);
-                if (t.n == 0) continue;
+                if (t.n == 0) {
+                    if (rank == 0) wide_arrive(&bars.claim_ask, 0);
+                    continue;
+                }
+                const int asks = t.first + max(0, t.n - kWideAhead);
                 if (t.down && t.z != ready) {
                     if (!wide_ready(w.done + t.z, (unsigned)count * 2 * kWideEpiWarps, &bars.aborted, p.status)) goto done;
                     ready = t.z;
@@ -174,6 +231,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                 const uint32_t bytes = 2 * (128 * 128 + (t.down ? kDownRows : 128) * 64 + 3 * kMxTileBytes);
                 const int chunk = 2 * t.z + (int)rank, row = chunk * (t.down ? p.cap : kb);
                 for (int j = t.first; j < t.first + t.n; ++j, ++fill) {
+                    if (rank == 0 && j == asks) wide_arrive(&bars.claim_ask, 0);
                     if (fill >= kWideStages && !mx_wait(&bars.empty[ring.stage], ring.phase ^ 1, &bars.aborted, p.status)) goto done;
                     uint8_t *st = smem + ring.stage * kWideStageBytes;
                     if (rank == 0) mbar_expect_tx(&bars.full[ring.stage], bytes);
@@ -186,9 +244,9 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     } else if (warp == 2) {   // weights
         if (elect_one()) {
             const uint32_t full0 = map_to_cta(smem_u32(&bars.full[0]), 0);
-            MxRing ring;
+            MxRing ring, claims;
             int fill = 0, ahead = blockIdx.x;
-            for (int i = pair; i < items; i += pairs) {
+            for (int i; (i = wide_next<false>(&bars, claims, p.status)) < items;) {
                 const WideItem t = wide_item<DB>(w, count, i);
                 const CUtensorMap *m = t.down ? &tm_d : &tm_gu, *ms = t.down ? &tm_ds : &tm_gus;
                 // Gate/up: this CTA's half of the group.  Down: rows of W_down from where they stand, which may run into the next group's (columns
@@ -213,9 +271,9 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             const uint32_t base = smem_u32(smem), tmem = bars.tmem;
-            MxRing ring;
+            MxRing ring, claims;
             int turn = 0;
-            for (int i = pair; i < items; i += pairs) {
+            for (int i; (i = wide_next<false>(&bars, claims, p.status)) < items;) {
                 const WideItem t = wide_item<DB>(w, count, i);
                 if (t.n == 0) continue;
                 uint32_t idesc[4];
@@ -243,14 +301,21 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             }
         }
     } else if (warp == 3) {
-        if (p.fold) mx_check(p.support, p.entries, p.k, p.G, blockIdx.x, gridDim.x, p.status);
+        if (rank == 0) {
+            if (claimer) wide_claim(&bars, w.next, (int)first, items, p.status);
+        } else if (p.fold) {
+            mx_check(p.support, p.entries, p.k, p.G, pair, pairs, p.status);
+        }
     } else {
         const int quarter = warp & 3, half = (warp >> 2) - 1;      // lanes and half of the columns
         const uint32_t empty0 = map_to_cta(smem_u32(&bars.acc_empty), 0);
         const uint32_t acc = bars.tmem + ((uint32_t)(quarter * 32) << 16);
+        MxRing claims;
         int turn = 0;
-        for (int i = pair; i < items; i += pairs) {
+        for (;;) {
             __syncwarp();      // lanes without a token skip parts of an item
+            const int i = wide_next<true>(&bars, claims, p.status);
+            if (i >= items) break;
             const WideItem t = wide_item<DB>(w, count, i);
             const int token = t.z * kWideTokens + (int)rank * 128 + quarter * 32 + lane;
             if (!t.down) {
@@ -263,7 +328,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
                         member = ld_dep(reinterpret_cast<const int32_t *>(p.mask) + 4 * (size_t)token + (g >> 5)) >> (g & 31) & 1;
                 }
                 __syncwarp();
-                if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
+                if (!__all_sync(0xffffffffu, mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status))) break;
                 tc_fence_after();
                 uint32_t v[4][32];
 #pragma unroll
@@ -302,7 +367,7 @@ mx_wide_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__
             } else {
                 uint32_t v[DB][32];
                 if (t.n > 0) {
-                    if (!mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status)) break;
+                    if (!__all_sync(0xffffffffu, mx_wait(&bars.acc_full, turn & 1, &bars.aborted, p.status))) break;
                     tc_fence_after();
 #pragma unroll
                     for (int b = 0; b < DB; ++b) tc_ld32(acc + half * kDownRows + 32 * b, v[b]);
@@ -368,8 +433,10 @@ done:
     // the last pair to end clears the counters for the next call
     if (threadIdx.x == 0 && rank == 0) {
         __threadfence();
-        if (atomicAdd(w.done + w.ztiles, 1u) == (unsigned)pairs - 1)
+        if (atomicAdd(w.done + w.ztiles, 1u) == (unsigned)pairs - 1) {
             for (int z = 0; z <= w.ztiles; ++z) w.done[z] = 0;
+            *w.next = 0;
+        }
     }
 }
 
@@ -423,7 +490,7 @@ cs_status launch_mx_wide(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, 
     WideArgs w;
     w.p = args;
     w.ztiles = (B + kWideTokens - 1) / kWideTokens;
-    w.partial = plan->mx_partial; w.done = plan->mx_done;
+    w.partial = plan->mx_partial; w.next = plan->mx_done; w.done = plan->mx_done + kMxDoneOffset;
     w.down_codes = L->down_codes; w.down_scales = L->down_scales;
     w.whole = reinterpret_cast<uintptr_t>(args.out) % 32 == 0;
     // Output columns of a down item: the width whose rounds over the pairs cost least (13B shape, 2048 tokens: 160 items of 256 are three rounds, 216

@@ -420,6 +420,61 @@ def test_ffn_many_calls_back_to_back(B, d, G, k):
         p.plan.close()
 
 
+def test_ffn_large_batches_on_two_streams():
+    """Two plans whose batches take the persistent launch, side by side on streams of different priority and beside other work that comes and goes."""
+    ps = [Problem(200, 512, 112, 28, False, seed=1), Problem(700, 768, 24, 9, True, seed=2)]
+    want = [p.run() for p in ps]
+    for p, w in zip(ps, want):
+        p.check(w)
+    low, high = torch.cuda.Stream.priority_range()
+    streams = [torch.cuda.Stream(priority=low), torch.cuda.Stream(priority=high)]
+    third, a = torch.cuda.Stream(), randn(gen(8), 2048, 2048)
+    outs = [torch.zeros_like(w) for w in want]
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for _ in range(30):
+        for o in outs:
+            o.fill_(7)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            with torch.cuda.stream(third):
+                a @ a
+            for p, s, o in zip(ps, streams, outs):
+                with torch.cuda.stream(s):
+                    p.run(out=o)
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            wrong += (o != w).sum()
+    assert int(wrong) == 0
+    for p in ps:
+        assert p.plan.device_status() == 0
+        p.plan.close()
+
+
+@pytest.mark.parametrize("sms", [16, 64])
+@pytest.mark.parametrize("B,d,G,k,shared", [(300, 1024, 40, 12, False), (200, 512, 112, 28, False), (1100, 640, 24, 9, True), (1500, 512, 60, 20, False)])
+def test_ffn_large_batches_on_a_part_of_the_device(B, d, G, k, shared, sms):
+    """A launch of which some SMs' worth of CTAs has room at a time: its items are done by those that run."""
+    green = pytest.importorskip("torch.cuda.green_contexts")
+    if not green.SUPPORTED:
+        pytest.skip("torch without green contexts")
+    p = Problem(B, d, G, k, shared, seed=6)
+    want = p.run()
+    p.check(want)
+    torch.cuda.synchronize()
+    part = green.GreenContext.create(sms, 0)
+    stream = part.Stream()
+    out = torch.zeros_like(want)
+    for _ in range(3):
+        out.fill_(7)
+        torch.cuda.synchronize()
+        p.run(out=out, stream=stream)
+        stream.synchronize()
+        assert p.plan.device_status() == 0
+        assert torch.equal(out, want)
+    p.plan.close()
+    del part        # not before its stream's last use
+
+
 def test_ffn_refusals():
     p = Problem(8, 256, 4, 2, False)
     with pytest.raises(ValueError):
