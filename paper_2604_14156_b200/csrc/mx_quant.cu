@@ -255,20 +255,21 @@ pack_tiles_kernel(const uint8_t *__restrict__ c0, const uint8_t *__restrict__ s0
     }
 }
 
-bool fits(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 && rows * ((cols + 31) / 32) * 4 < (int64_t)1 << 31; }
+int64_t blocks_of(int64_t cols) { return (cols + 31) / 32; }      // 64 bits: cols may be the largest int32
+bool fits(int64_t rows, int64_t cols) { return rows > 0 && cols > 0 && rows * blocks_of(cols) * 4 < (int64_t)1 << 31; }
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 cs_status status_of(cudaError_t e) { return e == cudaSuccess ? CS_OK : CS_ERR_CUDA; }
 
 template <typename T> cs_status quantize(const T *w, int rows, int cols, int64_t ld, bool transpose, uint8_t *codes, uint8_t *scales, cudaStream_t st) {
     if (transpose) {
-        const int nb = (rows + 31) / 32;
+        const int nb = (int)blocks_of(rows);
         const dim3 grid((cols + kTCols - 1) / kTCols, (nb + kTBlocks - 1) / kTBlocks);
         if (grid.y > 65535) return CS_ERR_SHAPE;
         const bool vec = cols % 2 == 0 && ld % 2 == 0 && aligned(w, 2 * sizeof(T));
         return status_of(launch_pdl(true, vec ? quantize_cols_kernel<T, true> : quantize_cols_kernel<T, false>, grid, dim3(32 * kTBlocks), 0, st, w, rows,
                                     cols, ld, nb, codes, scales));
     }
-    const uint32_t nb = (cols + 31) / 32;
+    const uint32_t nb = (uint32_t)blocks_of(cols);
     const int64_t parts = (int64_t)rows * nb * 4;
     const dim3 grid((unsigned)((parts + kQThreads * kQUnroll - 1) / (kQThreads * kQUnroll)));
     const bool vec = cols % 8 == 0 && (ld * sizeof(T)) % 16 == 0 && aligned(w, 16);
@@ -277,7 +278,7 @@ template <typename T> cs_status quantize(const T *w, int rows, int cols, int64_t
 }
 
 template <typename T> cs_status dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, T *w, int64_t ld, cudaStream_t st) {
-    const uint32_t nb = (cols + 31) / 32;
+    const uint32_t nb = (uint32_t)blocks_of(cols);
     const int64_t parts = (int64_t)rows * nb * 4;
     const dim3 grid((unsigned)((parts + kQThreads * kQUnroll - 1) / (kQThreads * kQUnroll)));
     const bool vec = cols % 8 == 0 && (ld * sizeof(T)) % 16 == 0 && aligned(w, 16);

@@ -78,6 +78,29 @@ def test_quantize_strided_and_unaligned(transpose):
     assert (out[:, :10] == 7).all() and (out[:, 80:] == 7).all()
 
 
+@pytest.mark.parametrize("cols", [2 ** 31 - 1, 2 ** 31 - 8])
+def test_quantize_the_longest_row(cols):
+    """A row whose blocks, but not whose rounded-up length, can be counted in 32 bits."""
+    w = torch.zeros((1, cols), dtype=torch.bfloat16, device=DEV)
+    w[0, :100] = randn(gen(11), 100).bfloat16()
+    w[0, -100:] = randn(gen(12), 100).bfloat16()
+    codes, scales = cs.cs_mx_quantize(w)
+    nb = 2 ** 26
+    assert scales.shape == (1, nb) and codes.shape == (1, 16 * nb)
+    for at, n in ((0, 128), ((nb - 4) * 32, cols - (nb - 4) * 32)):
+        v, byte = R.quantize4(w[:, at:at + n])
+        assert torch.equal(scales.view(torch.uint8)[:, at // 32:at // 32 + 4], byte)
+        assert torch.equal(R.codes4(codes[:, at // 2:at // 2 + 64]), v)
+    assert int(scales.view(torch.uint8)[:, 4:-4].max()) == 0 and int(codes[:, 64:-64].max()) == 0
+    back = torch.full((1, cols), 7.0, dtype=torch.bfloat16, device=DEV)
+    cs.cs_mx_dequantize(codes, scales, cols, out=back)
+    assert torch.equal(back[0, -64:].double(), R.values4(codes[:, -256:], scales[:, -16:])[0, :cols - (nb - 16) * 32][-64:])
+    assert int(torch.count_nonzero(back[:, 128:-128])) == 0
+    del w, codes, scales, back
+    binding._matrix_templates.clear()
+    torch.cuda.empty_cache()
+
+
 def test_quantize_refusals():
     w = randn(gen(1), 64, 64)
     with pytest.raises(ValueError):
