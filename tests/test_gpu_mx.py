@@ -198,6 +198,28 @@ def test_norm_rows_of_zeros_nan_and_infinity():
     plan.close()
 
 
+@pytest.mark.parametrize("B", [1, 70, 900])
+def test_norm_reads_a_gamma_that_the_call_ahead_writes(B):
+    d = 4096
+    g = gen(B)
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    x = randn(g, B, d)
+    gammas = [cs.cs_mx_quantize(1 + 0.2 * randn(g, 1, d)) for _ in range(2)]
+    rows = [cs.cs_mx_dequantize(*q, d, torch.float32) for q in gammas]
+    torch.cuda.synchronize()
+    want = [cs.cs_mx_norm(plan, x, r[0])[1].view(torch.uint8) for r in rows]
+    assert not torch.equal(*want)
+    torch.cuda.synchronize()
+    row = torch.empty((1, d), device=DEV)
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for i in range(200):
+        cs.cs_mx_dequantize(*gammas[i % 2], d, out=row)
+        q = cs.cs_mx_norm(plan, x, row[0])[1]
+        wrong += (q.view(torch.uint8) != want[i % 2]).sum()
+    assert int(wrong) == 0
+    plan.close()
+
+
 def test_norm_refusals():
     plan = cs.Plan(256, 128, 128, 1, 1, 0, "mx4", 4, 1e-5)
     x = randn(gen(1), 4, 256)
