@@ -356,7 +356,8 @@ cs_status cs_mx_quantize(const void *w, int32_t dtype, int32_t rows, int32_t col
                          uint8_t *codes, uint8_t *scales, void *stream);
 
 /* The values codes and scales stand for, as f32 or bf16 (exact in both, but for magnitudes of 2^128 and more, which become
- * infinities: those above 3.5 * 2^126 are quantised to 2^128), rows of `ld` >= cols elements.  Refusals as above. */
+ * infinities: those above 3.5 * 2^126 are quantised to 2^128), rows of `ld` >= cols elements.  Refusals as above.  What it
+ * writes may be a parameter of the calls right behind it: it counts as an ordinary kernel there. */
 cs_status cs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int32_t rows, int32_t cols, int32_t dtype, void *w,
                            int64_t ld, void *stream);
 

@@ -603,7 +603,7 @@ def cs_mx_quantize(w, transpose: bool = False, codes=None, scales=None, stream=N
 
 
 def cs_mx_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, stream=None):
-    """The values [rows, cols] of cs_mx_quantize's codes and scales, as f32 or bf16."""
+    """The values [rows, cols] of cs_mx_quantize's codes and scales, as f32 or bf16.  They may be the weights of the call right behind."""
     lib = _lib or load_library()
     device = _device_index()
     rows, nb = codes.shape[0], -(-cols // 32)

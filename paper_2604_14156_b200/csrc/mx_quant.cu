@@ -186,9 +186,9 @@ __device__ __forceinline__ void unpack_e2m1(uint32_t q, float s, float (&v)[8]) 
     }
 }
 
+// Does not trigger the launch behind it: what it writes are weights, which this library's other calls may read ahead of their wait (parameters, cs.h).
 template <typename T, bool VEC> __global__ void __launch_bounds__(kQThreads)
 dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols, uint32_t nb, T *__restrict__ w, int64_t ld) {
-    pdl_launch_dependents();
     pdl_wait();
     const uint32_t parts = (uint32_t)rows * nb * 4;
     const uint32_t base = blockIdx.x * (kQThreads * kQUnroll) + threadIdx.x;

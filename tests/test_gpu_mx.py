@@ -604,3 +604,31 @@ def test_two_layers_of_a_decode_step(B, oracle):
         assert ((out.double() - want).abs() <= tol).all()
         delta = out
     plan.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_dequantised_weights_go_straight_into_the_other_ffn(dtype):
+    """All three matrices dequantised in front of the call that takes them as parameters, into the same place for two layers in turn."""
+    d, G, k, B = 256, 6, 2, 3
+    g = gen(31)
+    plan = cs.Plan(d, 128 * G, 128, 1, k, 0, dtype, B, 1e-5)
+    sources = [[cs.cs_mx_quantize(randn(g, 128 * G, d) / 16) for _ in range(3)] for _ in range(2)]
+    w = [torch.empty((128 * G, d), dtype=dtype, device=DEV) for _ in range(3)]
+    layer = cs.Layer(plan, torch.zeros((1, d), device=DEV), torch.zeros((1, G), device=DEV), *w, 1.0)
+    h = randn(g, B, d)
+    support = torch.tensor([[0, 3], [1, 3], [2, 5]], dtype=torch.int32, device=DEV)
+    want = []
+    for source in sources:
+        for q, out in zip(source, w):
+            cs.cs_mx_dequantize(*q, d, out=out)
+        torch.cuda.synchronize()
+        want.append(cs.cs_ffn_exec(plan, layer, h, support))
+        torch.cuda.synchronize()
+    assert not torch.equal(*want)
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for i in range(300):
+        for q, out in zip(sources[i % 2], w):
+            cs.cs_mx_dequantize(*q, d, out=out)
+        wrong += (cs.cs_ffn_exec(plan, layer, h, support) != want[i % 2]).sum()
+    assert int(wrong) == 0 and plan.device_status() == 0
+    plan.close()
