@@ -21,6 +21,8 @@
 // accumulators are added over distributed shared memory in a fixed order.
 #include <stdio.h>
 
+#include <atomic>
+
 #include "mx_core.cuh"
 
 namespace cs {
@@ -411,14 +413,11 @@ cs_status prepare_mx_ffn(cs_plan *plan) {
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxSmemOne) != cudaSuccess || prefer_shared(k) != cudaSuccess)
             return CS_ERR_CUDA;
     // Clusters stand within a part of the device, so fewer of them fit than its SMs suggest (of 8 CTAs 15, not 18), and one more is another round.
-    // (Asked once per device: a property of it, and 0.1 ms of a plan's creation.)
-    static int clusters[64][kMxMaxCluster + 1];
-    const bool kept = plan->device < 64 && clusters[plan->device][kMxMaxCluster] != 0;
+    // (Asked once per device: a property of it, and 0.1 ms of a plan's creation.  Threads that create plans at once may each ask, and get the same answer.)
+    static std::atomic<int> clusters[64][kMxMaxCluster + 1];      // 0: not asked yet
     for (int cs = 1; cs <= kMxMaxCluster; ++cs) {
-        if (kept) {
-            plan->mx_clusters[cs] = clusters[plan->device][cs];
-            continue;
-        }
+        if (plan->device < 64) plan->mx_clusters[cs] = clusters[plan->device][cs].load(std::memory_order_relaxed);
+        if (plan->mx_clusters[cs] != 0) continue;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         cfg.gridDim = dim3(cs, 1024); cfg.blockDim = dim3(kMxThreads); cfg.dynamicSmemBytes = kMxSmemOne - 2048;
@@ -426,7 +425,7 @@ cs_status prepare_mx_ffn(cs_plan *plan) {
         attr[0].val.clusterDim.x = cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = 1;
         if (cudaOccupancyMaxActiveClusters(&plan->mx_clusters[cs], mx_gateup_kernel, &cfg) != cudaSuccess) return CS_ERR_CUDA;
-        if (plan->device < 64) clusters[plan->device][cs] = plan->mx_clusters[cs];
+        if (plan->device < 64) clusters[plan->device][cs].store(plan->mx_clusters[cs], std::memory_order_relaxed);
     }
     return prefer_shared(mx_list_kernel) == cudaSuccess ? prepare_mx_wide(plan) : CS_ERR_CUDA;
 }

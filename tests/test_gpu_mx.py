@@ -520,6 +520,34 @@ def test_ffn_large_batches_on_a_part_of_the_device(B, d, G, k, shared, sms):
     del part        # not before its stream's last use
 
 
+def test_plans_created_by_several_threads_at_once():
+    """The FFN's launch shapes come from the plan: plans created side by side give what one created alone gives."""
+    import threading
+    p = Problem(64, 1024, 16, 5, False, seed=7)
+    want = p.run()
+    torch.cuda.synchronize()
+    got, errors = [], []
+
+    def work():
+        try:
+            for _ in range(5):
+                plan = cs.Plan(1024, 2048, 128, 1, 5, 0, "mx4", 64, 1e-5)
+                stream = torch.cuda.Stream()
+                with torch.cuda.stream(stream):
+                    got.append(cs.cs_mx_ffn(plan, p.layer, p.q, p.s, p.support))
+                stream.synchronize()
+                plan.close()
+        except Exception as e:
+            errors.append(e)
+    threads = [threading.Thread(target=work) for _ in range(6)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors and len(got) == 30 and all(torch.equal(o, want) for o in got)
+    p.plan.close()
+
+
 def test_ffn_refusals():
     p = Problem(8, 256, 4, 2, False)
     with pytest.raises(ValueError):
