@@ -13,6 +13,8 @@
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library neither frees nor
  *     keeps it after the call's work has run.  cs_config / cs_layer structs are HOST memory and
  *     are read before the call returns.
+ *   - A plan belongs to the device that is current when it is created: its scratch is there, and its calls are made with that
+ *     device current.
  *   - Calls only enqueue work on `stream` (a cudaStream_t passed as void*, NULL = default
  *     stream) and return without synchronising.  A plan must not be used from two streams at
  *     once: its scratch is shared by all calls.

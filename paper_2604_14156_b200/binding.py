@@ -183,6 +183,7 @@ class Plan:
         if st != 0:
             raise CSError(st, "cs_plan_create")
         self.handle = handle
+        self.device = torch.cuda.current_device()      # where its scratch is
 
     def outputs(self, B: int, device):
         """New (support [B,k], z [B,k], resid [B]) for a call's outputs.  Allocated like templates that are kept per batch
@@ -519,6 +520,14 @@ def _device_index() -> int:
     return _current_device() if _current_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
+def _plan_device(plan: Plan) -> int:
+    """The current device, which has to be the plan's: its scratch is there."""
+    device = _device_index()
+    if device != plan.device:
+        raise ValueError(f"the plan is on cuda:{plan.device}, but the current device is cuda:{device}")
+    return device
+
+
 def _checked(t, dtypes, name: str, shape, device: int, optional: bool = False) -> Optional[int]:
     """The pointer of a contiguous tensor of one of `dtypes` and of this shape on the device whose stream the call uses.  The usual case
     is one line (half a microsecond a tensor is most of what a small call takes on the host)."""
@@ -630,7 +639,7 @@ class MxLayer:
 
     def __init__(self, plan: Plan, gate, up, down, stream=None):
         d, d_ff = plan.d, plan.d_ff
-        device = _device_index()
+        device = _plan_device(plan)
 
         def matrix(pair, name, rows, cols):
             return _MxMatrix(_checked(pair[0], (torch.uint8,), name + " codes", (rows, cols // 2), device),
@@ -650,7 +659,7 @@ def cs_mx_norm(plan: Plan, x, gamma=None, delta=None, want_n: bool = False, x_ou
     of row r, block b stands at [r // 128, b // 4, r % 32, r % 128 // 32, b % 4]."""
     B, d, dev = x.shape[0], plan.d, x.device
     rows = (B, d)
-    device = _device_index()
+    device = _plan_device(plan)
     px = _checked(x, _FLOATS, "x", rows, device)
     pd = _checked(delta, _FLOATS, "delta", rows, device, True)
     pg = _checked(gamma, (torch.float32,), "gamma", (d,), device, True)
@@ -674,7 +683,7 @@ def cs_mx_norm(plan: Plan, x, gamma=None, delta=None, want_n: bool = False, x_ou
 
 def _mx_ffn(call, name, plan: Plan, layer: MxLayer, q, s, support, support_shape, out, stream):
     B, d = q.shape[0], plan.d
-    device = _device_index()
+    device = _plan_device(plan)
     # before the output: a template made for a tensor of another device would serve the calls after this one
     pq = _checked(q, _BYTES, "q", (B, d), device)
     ps = _checked(s, _BYTES, "s", (-(-B // 128), d // 128, 32, 4, 4), device)

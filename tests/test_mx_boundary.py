@@ -107,3 +107,17 @@ def test_refused_norm_and_matrix_calls_leave_no_output_template(monkeypatch):
         with pytest.raises((TypeError, ValueError)):
             call()
     assert plan._templates == {} and binding._matrix_templates == before
+
+
+def test_a_plan_of_another_device_is_refused(monkeypatch):
+    """Its scratch is there, while stream and tensors would be here."""
+    monkeypatch.setattr(binding, "_device_index", lambda: 1)
+    monkeypatch.setattr(binding, "_checked", lambda *args: 1 << 20)      # tensors of the current device
+    plan, layer = _HostPlan(), type("layer", (), dict(ref=None))
+    plan.d_ff = 512
+    q = torch.zeros((8, 256), dtype=torch.float8_e4m3fn)
+    pair = (torch.zeros((512, 128), dtype=torch.uint8), torch.zeros((512, 8), dtype=torch.uint8))
+    for call in (lambda: binding.cs_mx_norm(plan, torch.zeros((8, 256))), lambda: binding.cs_mx_ffn(plan, layer, q, None, None, stream=0),
+                 lambda: binding.cs_mx_ffn_shared(plan, layer, q, None, None, stream=0), lambda: binding.MxLayer(plan, pair, pair, pair)):
+        with pytest.raises(ValueError, match="plan is on"):
+            call()
