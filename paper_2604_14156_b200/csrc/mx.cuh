@@ -58,11 +58,16 @@ __device__ __forceinline__ uint16_t pack_e4m3x2(float a, float b) {
     return r;
 }
 
-// silu(gate) up = gate up / (1 + 2^(-gate log2 e)).  The bare approximate exponential and reciprocal (their operands need no care for subnormals:
-// 1 + e >= 1, and an e that overflows gives 0): about 2^-20 of the result, against the 2^-4 of the rounding that follows.
+// silu(gate) up = gate up / (1 + 2^t), t = -gate log2 e, by the bare approximate exponential (2^-22) and reciprocal (2^-23).  t in one f32 is off by up to
+// 2^-19 at 2^6, and the exponential by as much of itself, so 2^t is corrected by what t lost: with the roundings of the sum and the two products
+// less than 2^-20 of the result, against the 2^-4 of the rounding that follows.  Clamped where 2^t is below 2^-128, or above 2^126, whose reciprocal counts
+// as 0 (gates below -87.3): so that nothing overflows in between.  A NaN comes back through the last product.
 __device__ __forceinline__ float swiglu(float gate, float up) {
+    const float x = fminf(fmaxf(-gate, -89.f), 88.f), t = 1.44269502f * x;
+    const float lost = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -t));
     float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * gate));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    e = fmaf(e * 0.693147181f, lost, e);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return gate * r * up;
 }

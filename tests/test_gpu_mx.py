@@ -520,6 +520,52 @@ def test_ffn_large_batches_on_a_part_of_the_device(B, d, G, k, shared, sms):
     del part        # not before its stream's last use
 
 
+@pytest.mark.parametrize("B", [100, 600, 3000])
+def test_ffn_activations_are_rounded_within_their_bound(B):
+    """W_down = 1, so that the output is a^ itself (four significant bits, exact in bf16), and gates that are exact in f32: wherever silu(gate) up is further
+    than 2^-20 of itself from the middle of two e4m3 values, and its block's largest from a border of the scale, a^ is the nearest value."""
+    g, d = gen(B), 128
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    levels = torch.tensor([1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=DEV)
+    support = torch.zeros((B, 1), dtype=torch.int32, device=DEV)
+    down = cs.cs_mx_quantize(torch.eye(128, device=DEV), transpose=True)
+    up_w = torch.zeros((128, d), device=DEV)
+    up_w[:, 127] = 1.0
+    checked = 0
+    for _ in range(1 + 2000000 // (128 * B)):
+        # gate = sum over four blocks of 2^-4b x_b w_b: at most 6 + 12 bits
+        w = torch.zeros((128, d), device=DEV)
+        w[:, 0] = levels[torch.randint(6, (4,), generator=g, device=DEV)].repeat_interleave(32)      # near gates within a block of channels
+        for b in (1, 2, 3):
+            w[:, 32 * b] = levels[torch.randint(6, (128,), generator=g, device=DEV)] * (1 - 2 * torch.randint(2, (128,), generator=g, device=DEV))
+        gate = cs.cs_mx_quantize(w)
+        assert torch.equal(R.values4(*gate), w.double())
+        layer = cs.MxLayer(plan, gate, cs.cs_mx_quantize(up_w), down)
+        x = torch.zeros((B, d), device=DEV)
+        for b in range(4):
+            x[:, 32 * b] = (1 + torch.randint(8, (B,), generator=g, device=DEV) / 8) * 2.0 ** torch.randint(-2, 3, (B,), generator=g, device=DEV)
+        x[:, 0] *= (1 - 2 * (torch.rand((B,), generator=g, device=DEV) < 0.8).float()) * (x[:, 0] <= 12)
+        x[:, 127] = 1.0
+        q, e = x.to(torch.float8_e4m3fn), 127 - 4 * torch.arange(4, device=DEV).expand(B, 4)
+        e = torch.cat((e[:, :3], torch.full((B, 1), 127 - 12, device=DEV)), 1).to(torch.uint8)
+        assert torch.equal(q.float(), x)
+        real = x.double() * R.two_to(e.long() - 127).repeat_interleave(32, dim=1)
+        out = cs.cs_mx_ffn(plan, layer, q, R.tiles(e).view(torch.float8_e8m0fnu), support).double()
+        f, u = real @ w.double().t(), real @ up_w.double().t()
+        assert torch.equal(f.float().double(), f)
+        a = f / (1 + torch.exp(-f)) * u
+        v, step, s = R.round8(a)
+        near = 2.0 ** -20 * a.abs()
+        top = a.abs().reshape(B, -1, 32).amax(-1)
+        border = (top * (1 + 2.0 ** -20) > 448 * s) | (top * (1 - 2.0 ** -20) <= 224 * s)
+        sure = ((a / step - torch.floor(a / step) - 0.5).abs() * step > near) & ~border.repeat_interleave(32, dim=1)
+        assert (out == v)[sure].all(), (f[sure & (out != v)][:4].tolist(), int((sure & (out != v)).sum()))
+        checked += int((sure & (v != 0)).sum())
+    assert checked > 700000
+    assert plan.device_status() == 0
+    plan.close()
+
+
 def test_plans_created_by_several_threads_at_once():
     """The FFN's launch shapes come from the plan: plans created side by side give what one created alone gives."""
     import threading
