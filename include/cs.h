@@ -380,12 +380,14 @@ cs_status cs_mx_pack(const cs_plan *plan, const cs_mx_matrix *gate, const cs_mx_
 
 /*
  * What stands in front of the FFN of a layer:  h = x + delta, rounded to x's type (delta NULL: h = x);
- * n = h / sqrt(mean(h^2) + rms_eps) * gamma (gamma NULL: 1), in f32;  q, s = n in blocks of e4m3.
+ * n = h / sqrt(mean(h^2) + rms_eps) * gamma (gamma NULL: 1);  q, s = n in blocks of e4m3, the rounding of n itself (but where it
+ * stands within 2^-42 of itself of the middle of two values, or a block's largest of a border of the scale); n_out is n in f32,
+ * within 2^-22 of itself.
  *   x [B,d] f32 or bf16, delta [B,d] f32 or bf16 (the output of the block before), gamma [d] f32
  *   -> x_out [B,d] of x's type (may be x or NULL), n_out [B,d] f32 or NULL (what cs_sketch reads), q [B,d] e4m3 bytes,
  *   s [ceil(B/128), d/128, 512] bytes: the scale of row r, block b at byte (r % 32) * 16 + (r % 128 / 32) * 4 + b % 4 of tile
  *   (r / 128, b / 4), the order in which block-scaled tensor-core products read scales; scales of rows from B on are 0.
- * Magnitudes up to 2^60 (the sum of squares is formed in f32 by parts).  A NaN makes its row NaN, an infinity its block (the
+ * Magnitudes up to 2^60 (the mean square has to be an f32).  A NaN makes its row NaN, an infinity its block (the
  * rest of such a row is 0); rows keep to themselves.  Other than x_out = x, outputs overlap no input.
  * Pointers are 16-byte aligned.  No scratch of the plan is used.
  */

@@ -198,6 +198,59 @@ def test_norm_rows_of_zeros_nan_and_infinity():
     plan.close()
 
 
+def check_rounded_exactly(x, gamma, eps, q, s):
+    """q and s are the blocks of the true n, but where n is within 2^-42 of itself of the middle of two values, or the block's largest of the scale's border:
+    f64 has 2^-51 of n here, the kernel a root of one Newton step from 2^-22 (2^-43) and products whose errors are carried along (2^-46)."""
+    f = x.double()
+    n = f / torch.sqrt(f.square().mean(1, keepdim=True) + eps) * gamma.double()
+    v, step, scale = R.round8(n)
+    top = n.abs().reshape(x.shape[0], -1, 32).amax(-1)
+    sure = ~((top * (1 + 2.0 ** -42) > 448 * scale) | (top * (1 - 2.0 ** -42) <= 224 * scale))
+    got = R.untiles(s, x.shape[0], x.shape[1] // 32)
+    assert torch.equal(got[sure], scale[sure])
+    sure = sure.repeat_interleave(32, dim=1) & ((n / step - torch.floor(n / step) - 0.5).abs() * step > 2.0 ** -42 * n.abs())
+    value = q.double() * got.repeat_interleave(32, dim=1)
+    assert torch.equal(value[sure], v[sure]), int((value != v)[sure].sum())
+    assert sure.double().mean() > 0.99
+
+
+@pytest.mark.parametrize("B,d", [(1, 256), (3, 4096), (700, 4096), (700, 5120), (1300, 1152), (2500, 1280)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_rounds_the_true_value(B, d, dtype):
+    """Rows of which a few channels hold nearly all of the sum of squares."""
+    g = gen(B + d)
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    for hot in (1, 31, 1000):
+        x = (randn(g, B, d) * (1 + hot * (torch.rand((B, d), generator=g, device=DEV) < 0.01))).to(dtype)
+        gamma = 1 + 0.2 * randn(g, d)
+        _, q, s, _ = cs.cs_mx_norm(plan, x, gamma)
+        check_rounded_exactly(x, gamma, 1e-5, q, s)
+    plan.close()
+
+
+@pytest.mark.parametrize("B,d", [(1, 256), (2, 4096), (700, 4096), (700, 5120), (1300, 1152), (2500, 1280)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_next_to_the_middles(B, d, dtype):
+    """gamma chosen so that every n is within a unit or two of f32 of the middle of two e4m3 values, and the blocks' largest as near to a border of the scale."""
+    g = gen(3 * B + d)
+    x = (randn(g, 1, d) * (1 + 30 * (torch.rand((1, d), generator=g, device=DEV) < 0.01))).to(dtype)
+    x[x == 0] = 1
+    f = x.double()
+    r = 1 / torch.sqrt(f.square().mean(1, keepdim=True) + 1e-5)
+    # middles: (8 .. 15 + 1/2) 2^p under a largest of 448, which is 14 2^5
+    target = (8.5 + torch.randint(8, (1, d), generator=g, device=DEV)) * 2.0 ** torch.randint(-8, 5, (1, d), generator=g, device=DEV)
+    target[:, 5::32] = 448.0
+    target *= 2.0 ** torch.randint(-3, 4, (1, d // 32), generator=g, device=DEV).repeat_interleave(32, dim=1)
+    gamma = (target.double() / (f * r)).float()
+    ulp = 1 + 2.0 ** -23 * torch.randint(-2, 3, (1, d), generator=g, device=DEV)
+    gamma = (gamma.double() * ulp).float()[0].contiguous()
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    x = x.expand(B, d).contiguous()
+    _, q, s, _ = cs.cs_mx_norm(plan, x, gamma)
+    check_rounded_exactly(x, gamma, 1e-5, q, s)
+    plan.close()
+
+
 @pytest.mark.parametrize("B", [1, 70, 900])
 def test_norm_reads_a_gamma_that_the_call_ahead_writes(B):
     d = 4096
