@@ -627,7 +627,7 @@ def cs_mx_dequantize(codes, scales, cols: int, dtype=torch.bfloat16, out=None, s
         ptr, ld = _matrix(out, _FLOATS, "out", device)
         if out.shape != (rows, cols):
             raise ValueError(f"out must have shape {(rows, cols)}, got {tuple(out.shape)}")
-    st = lib.cs_mx_dequantize(pc, ps, rows, cols, _DTYPES[out.dtype], ptr, ld, _stream(stream))
+    st = lib.cs_mx_dequantize(pc, ps, rows, cols, _dtype_code(out, "out"), ptr, ld, _stream(stream))
     if st != 0:
         raise CSError(st, "cs_mx_dequantize")
     return out

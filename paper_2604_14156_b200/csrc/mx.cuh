@@ -51,12 +51,6 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
         "mov.b32 %0, {lo, hi};\n}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
     return r;
 }
-// Two floats as e4m3 bytes, the first in the lower.
-__device__ __forceinline__ uint16_t pack_e4m3x2(float a, float b) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-    return r;
-}
 
 // silu(gate) up = gate up / (1 + 2^t), t = -gate log2 e, by the bare approximate exponential (2^-22) and reciprocal (2^-23).  t in one f32 is off by up to
 // 2^-19 at 2^6, and the exponential by as much of itself, so 2^t is corrected by what t lost: with the roundings of the sum and the two products
