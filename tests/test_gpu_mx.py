@@ -251,6 +251,30 @@ def test_norm_next_to_the_middles(B, d, dtype):
     plan.close()
 
 
+@pytest.mark.parametrize("B,d", [(6, 256), (800, 4096), (2500, 1024), (1300, 1152)])
+@pytest.mark.parametrize("xt,dt", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.bfloat16, None)])
+def test_norm_rows_of_nan_and_infinity_keep_to_themselves(B, d, xt, dt):
+    g = gen(B + 1)
+    x, delta = randn(g, B, d).to(xt), None if dt is None else randn(g, B, d).to(dt)
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    want = cs.cs_mx_norm(plan, x, None, delta=delta, want_n=True)
+    x[1] = 0
+    x[2, 17] = float("nan")
+    x[B - 2, 200] = float("inf")
+    if dt is not None:
+        delta[1] = 0
+        delta[B // 2, d - 1] = float("nan")
+        delta[B - 1, 3] = -float("inf")
+    got = cs.cs_mx_norm(plan, x, None, delta=delta, want_n=True)
+    check_norm(x, None, delta, 1e-5, got)
+    same = torch.ones(B, dtype=torch.bool, device=DEV)
+    same[[1, 2, B // 2, B - 2, B - 1]] = False
+    for a, b in ((want[0], got[0]), (want[1].view(torch.uint8), got[1].view(torch.uint8)), (want[3], got[3])):
+        assert torch.equal(a[same], b[same])
+    assert (got[1][1].float() == 0).all() and plan.device_status() == 0
+    plan.close()
+
+
 @pytest.mark.parametrize("B", [1, 70, 900])
 def test_norm_reads_a_gamma_that_the_call_ahead_writes(B):
     d = 4096
@@ -617,6 +641,94 @@ def test_ffn_activations_are_rounded_within_their_bound(B):
     assert checked > 700000
     assert plan.device_status() == 0
     plan.close()
+
+
+# the paths that a batch can take: narrow with the list in the launch and with a list kernel; pairs, with the list in the launch (parts of the list, whole
+# lists) and with a list kernel
+PATHS = [(3, 256, 6, 3, False), (64, 512, 12, 5, False), (128, 384, 40, 20, False), (100, 256, 8, 3, True), (200, 512, 112, 28, False),
+         (300, 256, 10, 3, False), (300, 1024, 90, 12, False), (2000, 256, 12, 5, False), (2000, 1280, 10, 4, True), (1500, 512, 128, 40, False)]
+
+
+@pytest.mark.parametrize("B,d,G,k,shared", PATHS)
+def test_ffn_invalid_supports_on_every_path(B, d, G, k, shared):
+    p = Problem(B, d, G, k, shared, seed=8)
+    good = p.support.clone()
+    rows, sup = (1, p.support.view(1, k)) if shared else (B, p.support)
+    bad = torch.full((k,), -7, dtype=torch.int32, device=DEV)
+    bad[1], bad[2] = G // 2, G + 3
+    sup[rows - 1] = bad                      # the last row: one group
+    if rows > 2:
+        sup[0] = 1 << 30                     # the first: none
+        sup[1] = 1                           # the second: one, many times
+    out = p.run()
+    assert p.plan.device_status() == 4
+    m = torch.zeros((rows, G), dtype=torch.bool, device=DEV)
+    m.scatter_(1, good.view(rows, k).long(), True)
+    m[rows - 1] = False
+    m[rows - 1, G // 2] = True
+    if rows > 2:
+        m[0] = m[1] = False
+        m[1, 1] = True
+        assert (out[0] == 0).all()
+    want, tol = R.ffn(*p.operands(), m.expand(B, G).repeat_interleave(128, dim=1))
+    assert ((out.double() - want).abs() <= tol).all()
+    p.support.fill_(-5)
+    out.fill_(7)
+    assert (p.run(out=out) == 0).all() and p.plan.device_status() == 4
+    p.support.copy_(good)
+    p.check(p.run())                         # nothing of it stays
+    p.plan.close()
+
+
+@pytest.mark.parametrize("B,d,G,k,shared", PATHS)
+def test_ffn_rows_do_not_depend_on_their_neighbours(B, d, G, k, shared):
+    """Other rows' activations change, also to NaN, and their supports (the union stays, and with it the order of sums): a row's output does not."""
+    p = Problem(B, d, G, k, shared, seed=9)
+    g = gen(B)
+    if not shared:
+        p.support[: -(-G // k)] = torch.stack([torch.arange(i, i + k, device=DEV) if i + k <= G else torch.arange(G - k, G, device=DEV)
+                                               for i in range(0, G, k)])[:B].to(torch.int32)
+    want = p.run()
+    stay = torch.rand((B,), generator=g, device=DEV) < 0.5
+    stay[: -(-G // k)] = True
+    stay[B // 2] = B == 3
+    other = ~stay
+    _, q, s, _ = cs.cs_mx_norm(p.plan, randn(g, B, d) * 50)
+    q = q.view(torch.uint8)
+    byte = torch.where(stay[:, None], R.untiles(p.s, B, d // 32), R.untiles(s, B, d // 32))
+    q = torch.where(stay[:, None], p.q.view(torch.uint8), q)
+    p.q.view(torch.uint8).copy_(q)
+    p.s.view(torch.uint8).copy_(R.tiles((torch.log2(byte) + 127).to(torch.uint8)))
+    if not shared:
+        new = torch.rand((B, G), generator=g, device=DEV).topk(k, dim=1).indices.sort(dim=1).values.to(torch.int32)
+        p.support.copy_(torch.where(stay[:, None], p.support, new))
+    got = p.run()
+    p.check(got)
+    assert torch.equal(got[stay], want[stay])
+    if other.any():
+        r = int(torch.nonzero(other)[-1])
+        q = p.q.view(torch.uint8)
+        q[r, 17] = 0x7F
+        again = p.run()
+        same = torch.ones(B, dtype=torch.bool, device=DEV)
+        same[r] = False
+        assert torch.isnan(again[r]).all() and torch.equal(again[same], got[same])
+        q[r, 17] = 0
+        p.s.view(torch.uint8)[r // 128, 1, r % 32, r % 128 // 32, 2] = 255
+        again = p.run()
+        assert torch.isnan(again[r]).all() and torch.equal(again[same], got[same])
+    p.plan.close()
+
+
+@pytest.mark.parametrize("B,d,G,k,shared", PATHS)
+def test_ffn_scales_of_padding_rows_on_every_path(B, d, G, k, shared):
+    p = Problem(B, d, G, k, shared, seed=10)
+    want = p.run()
+    pad = R.tiles(torch.ones((B, d // 32), dtype=torch.uint8, device=DEV)) == 0
+    p.s.view(torch.uint8)[pad] = 255
+    assert torch.equal(p.run(), want)
+    p.check(want)
+    p.plan.close()
 
 
 def test_plans_created_by_several_threads_at_once():
