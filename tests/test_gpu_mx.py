@@ -363,6 +363,28 @@ class Problem:
         assert self.plan.device_status() == 0
 
 
+@pytest.mark.parametrize("d,G", [(128, 1), (640, 3), (1024, 16)])
+def test_pack_is_the_documented_order(d, G):
+    g = gen(d + G)
+    gate, up = (cs.cs_mx_quantize(randn(g, 128 * G, d) * torch.exp(2 * randn(g, 128 * G, 1))) for _ in range(2))
+    down = cs.cs_mx_quantize(randn(g, 128 * G, d) * torch.exp(2 * randn(g, 1, d)), transpose=True)
+    plan = cs.Plan(d, 128 * G, 128, 1, 1, 0, "mx4", 1, 1e-5)
+    got = [t.clone() for t in cs.MxLayer(plan, gate, up, down).tensors]
+    kb = d // 128
+
+    def tile_scales(s):           # [tiles, 128, 4] -> tile order
+        return torch.cat([R.tiles(x).reshape(1, 512) for x in s])
+    # gate_up: group, 128 columns, half of the channels: 64 rows of gate, the same 64 of up
+    c = torch.stack([m[0].reshape(G, 2, 64, kb, 64) for m in (gate, up)], 2).permute(0, 4, 1, 2, 3, 5).reshape(-1, 128, 64)
+    s = torch.stack([m[1].view(torch.uint8).reshape(G, 2, 64, kb, 4) for m in (gate, up)], 2).permute(0, 4, 1, 2, 3, 5).reshape(-1, 128, 4)
+    assert torch.equal(got[0], c.reshape(-1)) and torch.equal(got[1], tile_scales(s).reshape(-1))
+    # down: group, 128 rows
+    c = down[0].reshape(kb, 128, G, 64).permute(2, 0, 1, 3).reshape(-1, 128, 64)
+    s = down[1].view(torch.uint8).reshape(kb, 128, G, 4).permute(2, 0, 1, 3).reshape(-1, 128, 4)
+    assert torch.equal(got[2], c.reshape(-1)) and torch.equal(got[3], tile_scales(s).reshape(-1))
+    plan.close()
+
+
 TOKENS = [1, 2, 3, 15, 16, 17, 31, 33, 64, 65, 100, 112, 113, 127, 128, 129, 144, 200, 255, 256, 257, 300, 513]
 
 
