@@ -9,6 +9,13 @@ namespace cs {
 
 namespace {
 
+// A const __restrict__ pointer whose plain loads stay behind the wait: the launch ahead may have written what it points at, and through the parameter itself
+// they could be taken for loads of constant data and moved ahead of it (see ld_dep).
+template <typename T> __device__ __forceinline__ T *behind_wait(T *p) {
+    asm volatile("" : "+l"(p)::"memory");
+    return p;
+}
+
 constexpr int kQThreads = 256;
 constexpr int kQUnroll = 4;     // 16- or 32-byte chunks a thread has in flight
 
@@ -79,6 +86,7 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(kQThreads)
 quantize_rows_kernel(const T *__restrict__ w, int rows, int cols, int64_t ld, uint32_t nb, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
     pdl_launch_dependents();
     pdl_wait();
+    w = behind_wait(w);
     const uint32_t parts = (uint32_t)rows * nb * 4;      // the host bounds it by 2^31
     const uint32_t base = blockIdx.x * (kQThreads * kQUnroll) + threadIdx.x;
     Eight<T> v[kQUnroll];
@@ -120,6 +128,7 @@ quantize_cols_kernel(const T *__restrict__ w, int rows, int cols, int64_t ld, in
     __shared__ uint8_t st[kTCols][kTBlocks];
     pdl_launch_dependents();
     pdl_wait();
+    w = behind_wait(w);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * kTCols + 2 * lane, b = blockIdx.y * kTBlocks + warp, r0 = b * kMxBlock;
     Cell v[kMxBlock];
@@ -236,6 +245,8 @@ pack_tiles_kernel(const uint8_t *__restrict__ c0, const uint8_t *__restrict__ s0
                   int inner, int groups, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
     pdl_launch_dependents();
     pdl_wait();
+    c0 = behind_wait(c0); s0 = behind_wait(s0);
+    if (GATE_UP) { c1 = behind_wait(c1); s1 = behind_wait(s1); }
     const int64_t tile = blockIdx.x;
     const int half = GATE_UP ? (int)(tile & 1) : 0;
     const int64_t q = GATE_UP ? tile >> 1 : tile, g = q / inner;

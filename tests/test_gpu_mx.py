@@ -893,3 +893,67 @@ def test_dequantised_weights_go_straight_into_the_other_ffn(dtype):
         wrong += (cs.cs_ffn_exec(plan, layer, h, support) != want[i % 2]).sum()
     assert int(wrong) == 0 and plan.device_status() == 0
     plan.close()
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("d,cols", [(256, 256), (1152, 1151), (4096, 4093)])
+def test_quantising_what_the_call_ahead_writes(d, cols, transpose):
+    """norm -> quantise (whole chunks, and single elements of an odd width) -> dequantise, nothing in between, for two inputs in turn."""
+    B = 33
+    g = gen(d)
+    plan = cs.Plan(d, 128, 128, 1, 1, 0, "mx4", B, 1e-5)
+    xs = [randn(g, B, d) * (1 + i) + i for i in range(2)]
+    n = torch.empty((B, d), device=DEV)
+    lib, layer_in = plan.lib, [cs.cs_mx_norm(plan, x, want_n=True) for x in xs]
+    torch.cuda.synchronize()
+    want = []
+    for got in layer_in:
+        n.copy_(got[3])
+        torch.cuda.synchronize()
+        codes, scales = cs.cs_mx_quantize(n[:, :cols], transpose=transpose)
+        torch.cuda.synchronize()
+        want.append((codes, scales.view(torch.uint8), cs.cs_mx_dequantize(codes, scales, B if transpose else cols, torch.float32)))
+        torch.cuda.synchronize()
+    assert not torch.equal(want[0][0], want[1][0])
+    q, s = layer_in[0][1].view(torch.uint8).clone(), layer_in[0][2].view(torch.uint8).clone()
+    codes, scales, back = (torch.empty_like(t) for t in want[0])
+    stream = torch.cuda.current_stream().cuda_stream
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for i in range(200):
+        assert lib.cs_mx_norm(plan.handle, xs[i % 2].data_ptr(), 0, None, 0, None, B, None, n.data_ptr(), q.data_ptr(), s.data_ptr(), stream) == 0
+        cs.cs_mx_quantize(n[:, :cols], transpose=transpose, codes=codes, scales=scales)
+        cs.cs_mx_dequantize(codes, scales, B if transpose else cols, out=back)
+        for a, b in zip((codes, scales, back), want[i % 2]):
+            wrong += (a != b).sum()
+    assert int(wrong) == 0
+    plan.close()
+
+
+def test_packing_what_the_calls_ahead_write():
+    """quantise three matrices, pack, FFN, nothing in between, for two layers in turn in the same place."""
+    d, G, k, B = 256, 4, 2, 5
+    g = gen(41)
+    plan = cs.Plan(d, 128 * G, 128, 1, k, 0, "mx4", B, 1e-5)
+    sources = [[randn(g, 128 * G, d) / 16 for _ in range(3)] for _ in range(2)]
+    _, q, s, _ = cs.cs_mx_norm(plan, randn(g, B, d))
+    support = torch.tensor([[0, 3], [1, 2], [1, 3], [0, 1], [2, 3]], dtype=torch.int32, device=DEV)
+    room = [cs.cs_mx_quantize(w, transpose=i == 2) for i, w in enumerate(sources[0])]
+    layer = cs.MxLayer(plan, *room)
+    matrices = [binding._MxMatrix(c.data_ptr(), e.data_ptr()) for c, e in room]
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def run(source, wait):
+        for i, (w, (c, e)) in enumerate(zip(source, room)):
+            cs.cs_mx_quantize(w, transpose=i == 2, codes=c, scales=e)
+        wait()
+        assert plan.lib.cs_mx_pack(plan.handle, *(ctypes.byref(m) for m in matrices), *(t.data_ptr() for t in layer.tensors), stream) == 0
+        wait()
+        return cs.cs_mx_ffn(plan, layer, q, s, support)
+    want = [run(source, torch.cuda.synchronize) for source in sources]
+    assert not torch.equal(*want)
+    torch.cuda.synchronize()
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for i in range(200):
+        wrong += (run(sources[i % 2], lambda: None) != want[i % 2]).sum()
+    assert int(wrong) == 0 and plan.device_status() == 0
+    plan.close()
