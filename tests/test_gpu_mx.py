@@ -753,6 +753,12 @@ def test_ffn_scales_of_padding_rows_on_every_path(B, d, G, k, shared):
     p.plan.close()
 
 
+@pytest.mark.parametrize("B,d,G,k,shared", [(1, 4096, 40, 22, False), (16, 2048, 16, 7, False), (64, 1024, 40, 12, False), (128, 384, 40, 20, False), (100, 256, 8, 3, True)])
+def test_ffn_small_batches_on_a_part_of_the_device(B, d, G, k, shared):
+    """Clusters, and down CTAs that start beside gate/up's, where 16 SMs are all there is."""
+    test_ffn_large_batches_on_a_part_of_the_device(B, d, G, k, shared, 16)
+
+
 def test_plans_created_by_several_threads_at_once():
     """The FFN's launch shapes come from the plan: plans created side by side give what one created alone gives."""
     import threading
