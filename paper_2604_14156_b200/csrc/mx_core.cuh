@@ -29,7 +29,12 @@ cs_status prepare_mx_wide(cs_plan *plan);
 
 namespace {
 
-constexpr int kMxFoldEntries = 2048, kWideFoldEntries = 8192;   // up to this many support entries gate/up makes the list itself
+// Up to this many support entries (narrow, wide) the products' launch makes the list itself; beyond, mx_list_kernel does and leaves membership bits.  With a list
+// kernel and without, us, 22 of 86 groups of d = 4096: 64 tokens (1408 entries) 28.7 and 27.3, 93 (2046) 35.6 and 34.2, 94 35.7 and 34.2, 128 (2816) 39.7 and
+// 38.0; wide: 200 tokens (4400) 48.5 and 46.5, 372 (8184) 68.2 and 64.9, 400 (8800) 69.2 and 65.5, 2000 (44000) 206 and 192: for rows this long both limits
+// are early.  What speaks for one is the wide launch's search of a token's own entries, once a group, where rows are short: 32 of 64 of d = 1024, 200
+// tokens (6400) 27.7 and 30.3, 300 (9600) 33.6 and 33.9.
+constexpr int kMxFoldEntries = 2048, kWideFoldEntries = 8192;
 constexpr int kMxWBytes = 128 * 128;                 // a weight tile in shared memory
 constexpr int kMxWLoad = 128 * 64;                   // ... and in memory, which is what the barrier counts
 // One thread of a converged warp.  The compiler knows that an elect.sync branch is taken by a single thread; behind `lane == 0` it

@@ -14,8 +14,10 @@
 // What bounds it: HBM's 6.5 TB/s want 42 KB of weights in flight on every SM (a load takes 0.4 us from L2 and 0.9 from HBM, and 0.6 pass from the
 // end of a stage's products to the next load's issue and back), and weights take twice their size in shared memory: four stages of 25 KB, two CTAs to an SM
 // where there are that many, stream 5.0 TB/s at 64 tokens.  At one token the chain of latencies is all there is: list, first loads, products, exchange,
-// and again.  (Two warps issuing the products, loads asked of L2 ahead of the ring, one CTA with eight stages, and waits that poll gained nothing.)
-// 7B layer, 22 of 86 groups: 1 token 13.1 us, 3 tokens 17.5, 64 tokens 28.6, against 18.4, 48.6 and 72.3 MB of weights.
+// and again.  (Two warps issuing the products, loads asked of L2 ahead of the ring, and waits that poll gained nothing; one CTA with eight stages to
+// an SM was slower, but with 172 tiles on 148 SMs that is two rounds, and says nothing about the ring's depth.)
+// 7B layer, 22 of 86 groups: 1 token 13.0 us, 3 tokens 17.2, 64 tokens 29.4, against 18.4, 48.6 and 72.3 MB of weights (a captured graph, 14 layers in turn, so
+// that weights come from HBM; one layer again and again 12.4, 17.1 and 27.3).
 //
 // Work is split over a cluster where there are fewer tiles than SMs: each CTA of a cluster takes a part of the k blocks, and the
 // accumulators are added over distributed shared memory in a fixed order.
@@ -436,9 +438,10 @@ cs_status launch_mx_ffn(cs_plan *plan, const cs_mx_layer *L, const uint8_t *q, c
     const int cap = shared ? k : (int)min((int64_t)G, (int64_t)B * k);
     const int rows = shared ? 1 : B;
     // Which kernels.  Pairs take 256 tokens for the price of one, but a group to an item: few groups leave most pairs without one.  Narrow against wide, us:
-    // 22 of 86 groups of d = 4096, own supports, 100 tokens 38.4 and 45.8, 128 40.7 and 46.9, 129 (one CTA to an SM) 48.9 and 46.8, 200 55.5 and 48.2.
-    // Where gate/up's tiles fit the SMs once: 16 of 60 of 4096, 144 tokens 33.9 and 33.9, 176 36.1 and 34.3; 12 of 48 of 2048 25.2 and 26.1, 28.4 and 26.5;
-    // shared, 22 of 4096 25.0 and 29.1, 26.7 and 29.0; 54 of 5120 33.2 and 36.4, 34.9 and 36.8.
+    // 22 of 86 groups of d = 4096, own supports, 100 tokens 37.6 and 44.0, 128 39.7 and 45.6, 129 (one CTA to an SM) 48.7 and 45.6, 160 49.5 and 46.1; a shared
+    // support, 44 of 86, 128 26.9 and 31.0, 144 29.2 and 31.0, 160 30.0 and 30.9: there 128 is early.  Where gate/up's tiles fit the SMs once, own supports: 16
+    // of 60 of 4096, 128 tokens 28.7 and 33.2, 144 33.8 and 33.5, 160 34.2 and 33.7; 12 of 48 of 2048, 144 24.5 and 25.8, 160 25.0 and 25.6.  Shared: 22 of 4096
+    // 24.0 and 28.7 at 144 and at 160; 54 of 5120 33.7 and 36.5, 34.0 and 37.0: still ahead where the narrow kernels' tile ends.
     const bool wide = B > (2 * cap <= plan->sm_count ? kMxNarrowFew : kMxNarrowTokens);
     const int tile = min(kMxMaxTile, (B + 15) / 16 * 16);
     // Shared memory.  Where the weights are few (gate/up's tiles leave room for clusters of two on an SM each), one CTA of gate/up and two of down share an

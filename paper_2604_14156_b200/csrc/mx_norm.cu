@@ -3,7 +3,9 @@
 // A row is one pass of one CTA, eight elements a thread, kept in registers between the sum of squares and the quantisation, so HBM sees every byte
 // once.  mx_norm_kernel is a CTA per row: one round of latencies, for as many rows as are
 // resident at once.  More rows take mx_norm_rows_kernel, whose CTAs stay and have the next rows' bulk copies in flight while they work on one: with a CTA
-// per row the loads wait for the row before (2048 rows of 5120 bf16 took 21.5 us; now 18.9, 3.9 TB/s, the bound being instructions).
+// per row the loads wait for the row before (2048 rows of 5120 bf16 took 21.5 us; now 18.8 with inputs beyond L2, 3.9 TB/s; f32 26.3).  What bounds it is a
+// row's chain of latencies - load, sum, two reductions, a barrier, the scale, the store - with 18 warps to an SM: 31 instructions an element, issued at 2.1 a
+// cycle of the 4 that an SM can.
 #include "mx_core.cuh"
 
 namespace cs {

@@ -18,9 +18,10 @@
 // pairs the device has room for (items dealt out in advance would wait for pairs that have no SM yet).  All waits are bounded besides.  The gate/up
 // phase also asks L2 for the down weights.
 //
-// 2048 tokens of d = 5120, 27 of 108 groups (217 GFLOP): two launches of single CTAs 160 us, pairs 103, without spilled accumulators and with the union of the
-// supports inside the launch 83, one launch 79 (2.75 PFLOP/s; 90 over a second of load, at the clocks of the power cap).  An item's 40 k blocks take 12 us, of
-// which the products alone are 10.7, and 1 to 1.5 us pass from its last product to the next item's first.
+// 2048 tokens of d = 5120, 27 of 108 groups (217 GFLOP), back to back in a graph: two launches of single CTAs 160 us, pairs 103, without spilled accumulators and
+// with the union of the supports inside the launch 83, one launch 79, claimed items 75 (2.9 PFLOP/s; 91 over a second of load, at the clocks of the power
+// cap).  Where there are few items the first claim costs 1 us (777 tokens, 11 groups, 30.7 -> 31.5).  An item's 40 k blocks take 12 us, of which the
+// products alone are 10.7, and 1 to 1.5 us pass from its last product to the next item's first.
 #include <stdio.h>
 
 #include "mx_core.cuh"
