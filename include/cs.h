@@ -401,7 +401,8 @@ cs_status cs_mx_norm(cs_plan *plan, const void *x, int32_t x_dtype, const void *
  *   out[t] = sum_c a^[c] W_down[:, c], accumulated in f32 and rounded to bf16.
  *   q, s as cs_mx_norm leaves them (scales of rows from B on are read and may be anything), support [B,k] int32 as cs_ffn_exec
  *   (checked on the device; an index outside [0,G) counts for nothing) -> out [B,d] bf16.
- * Rows are independent, but weights that stand for NaN reach every token of a call whose union of supports holds their group.
+ * Rows are independent, but weights that stand for NaN reach every token of a call whose union of supports holds their group, and
+ * the order of a row's f32 sums goes by that union.  The same call on the same inputs gives the same bits.
  */
 cs_status cs_mx_ffn(cs_plan *plan, const cs_mx_layer *layer, const uint8_t *q, const uint8_t *s, const int32_t *support,
                     int32_t B, void *out, void *stream);
